@@ -335,7 +335,7 @@ struct Shared {
     Pack<N> entering[2][32];                   // the state that enters the tile
     uint64_t full[R], empty[R], ready[2];      // a stage is filled (or its tile dealt) / free; entering is there
     uint64_t dealt[R + 2];                     // for the joining warp: an entry of the queue is there
-    uint64_t mailed[2], credit[2];             // the maps are there; the CTAs behind have read the ones before last
+    uint64_t mailed[2], credit[2];             // the maps are there; each CTA behind has read the ones before last
     uint64_t told[4], taken[4];                // a run has been dealt to this CTA; rank 0: all CTAs know
     uint32_t inbox[4];
     Dealt queue[R + 2];                        // tile n's entry is rewritten once every warp is past tile n
@@ -501,7 +501,7 @@ __device__ __forceinline__ Map<N> compose(const Pack<N> (*A)[32], const Pack<N> 
     return m;
 }
 
-// The scan's last warp sends the tile's map to the tiles behind it in its run; the last tile of a run publishes the
+// The scan's last warp sends the tile's map to the CTAs behind it in its cluster; the last tile of a run publishes the
 // state behind it.  before, reset: the map of the warps before this one; own, r: this warp's.
 template <int N, bool BACK, int R>
 __device__ __forceinline__ void publish(const Params& p, Shared<N, BACK, R>& sm, const Dealt& t, const Map<N>& before, bool reset, const Map<N>& own,
@@ -516,11 +516,12 @@ __device__ __forceinline__ void publish(const Params& p, Shared<N, BACK, R>& sm,
         all.H = fma(all.A, sm.entering[side][lane], all.H);
         known = true;
     }
-    const int behind = min((int)(ranks - 1 - rank), p.chunks - 1 - t.order);
-    if (behind > 0) {
+    // All CTAs behind get it, those without a tile of this run too: a CTA gives its credit for a run once it has that run's
+    // mail, so none can give it twice before another has given it once, and a full count is one credit from each.
+    if (rank + 1 < ranks) {
         wait_on<true>(&sm.credit[side], (it >> 1 & 1) ^ 1, &sm.abort, p);
-        for (int k = 1; k <= behind; ++k)
-            send_map<N>(smem_u32(&sm.mail[side][rank][lane]), smem_u32(&sm.mailed[side]), rank + k, known, all);
+        for (uint32_t to = rank + 1; to < ranks; ++to)
+            send_map<N>(smem_u32(&sm.mail[side][rank][lane]), smem_u32(&sm.mailed[side]), to, known, all);
     }
     if (rank == ranks - 1 && t.run + 1 < p.runs) publish_state<N>(p, t.chain * p.runs + t.run, all.H, lane);
 }
@@ -731,8 +732,9 @@ __device__ __forceinline__ void deal_tiles(const Params& p, const Maps& maps, Sh
 
 // The joining warp.
 template <typename L, bool BACK, int R>
-__device__ __forceinline__ void join_tiles(const Params& p, Shared<L::N, BACK, R>& sm, uint32_t rank, int lane) {
+__device__ __forceinline__ void join_tiles(const Params& p, Shared<L::N, BACK, R>& sm, uint32_t rank, uint32_t ranks, int lane) {
     if (p.chunks == 1) return;
+    const uint32_t left = (uint32_t)p.chunks - (uint32_t)(p.runs - 1) * ranks;   // tiles of a chain's last run: of the ranks below
     Turn dealt{0, 0}, freed{0, 0};
     for (int it = 0;; ++it) {
         if (!wait_on(&sm.dealt[dealt.s], dealt.parity, &sm.abort, p)) break;
@@ -740,8 +742,12 @@ __device__ __forceinline__ void join_tiles(const Params& p, Shared<L::N, BACK, R
         const Dealt& t = sm.tile(it);
         if (t.order == kNoMore) break;
         Pack<L::N> state(0.f);
-        if (t.order >= 0) state = enter<L, L::N, BACK, R>(p, sm, t, it, rank, lane);
-        else if (rank > 0 && lane == 0) mbar_arrive(smem_u32(&sm.mailed[it & 1]));   // keeps the phases in step
+        if (t.order >= 0) {
+            state = enter<L, L::N, BACK, R>(p, sm, t, it, rank, lane);
+        } else {   // no use for the mail, but it keeps this CTA in step with those that have a tile
+            if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.mailed[it & 1]), left * 32 * (uint32_t)sizeof(Map<L::N>));
+            wait_on<true>(&sm.mailed[it & 1], it >> 1 & 1, &sm.abort, p);
+        }
         __syncwarp();
         if (lane < rank) mbar_arrive_cluster(map_to_cta(smem_u32(&sm.credit[it & 1]), lane));   // the mail has been read
         // every warp has read what was there two tiles ago once it has begun or left the tile before this one
@@ -842,7 +848,7 @@ __global__ void __launch_bounds__(kThreads, 2) linrec_forward_kernel(const __gri
     init_barriers(sm, rank, ranks);
     if (warp >= kWarps) {
         if (warp == kWarpDeal) deal_tiles<L, false, R>(p, maps, sm, ring, rank, ranks, lane);
-        else join_tiles<L, false, R>(p, sm, rank, lane);
+        else join_tiles<L, false, R>(p, sm, rank, ranks, lane);
         __syncwarp();
         cluster_sync_all();   // no CTA leaves while another may still send to it
         return;
@@ -953,7 +959,7 @@ __global__ void __launch_bounds__(kThreads, 2) linrec_backward_kernel(const __gr
     init_barriers(sm, rank, ranks);
     if (warp >= kWarps) {
         if (warp == kWarpDeal) deal_tiles<L, true, R>(p, maps, sm, ring, rank, ranks, lane);
-        else join_tiles<L, true, R>(p, sm, rank, lane);
+        else join_tiles<L, true, R>(p, sm, rank, ranks, lane);
         __syncwarp();
         cluster_sync_all();   // no CTA leaves while another may still send to it
         return;

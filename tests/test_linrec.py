@@ -103,6 +103,44 @@ def test_many_chains_whose_last_run_lacks_tiles(B, T, dtype):
     _compare(_pass(g, x, dy, dastac.GATE_LOG, h0, dl), *n, dastac.GATE_LOG, *s, None, dtype == torch.bfloat16)
 
 
+def _last_runs(g):
+    """(CTAs of a cluster, tiles of a chain's last run) as far as the workspace tells: it holds a row of states a run."""
+    B, T, D = g.shape
+    tiles, row = -(-T // dastac.LINREC_CHUNK), 256 if g.dtype == torch.bfloat16 else 128
+    chains = B * -(-D // (64 if g.dtype == torch.bfloat16 else 32))
+    runs = (dastac.linrec_workspace(g) - 256) // (chains * row)
+    return [(c, tiles - (runs - 1) * c) for c in range(1, 9) if -(-tiles // c) == runs]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("B,groups,tiles", [(14, 7, 13), (6, 7, 26), (4, 5, 26)])
+def test_last_runs_that_lack_tiles_for_some_of_a_cluster(B, groups, tiles, dtype):
+    """Chains whose last run has tiles for several CTAs of a cluster, which send one another their maps, and none for the
+    others: many such runs in a row, a few, and one.  Alone and with three calls at once, which leaves each cluster
+    more of them; the same bits every time."""
+    D, gate = groups * (64 if dtype == torch.bfloat16 else 32), dastac.GATE_LOG
+    (g, x, dy), (h0, dl), n, s = _inputs(B, B, tiles * 128 - 3, D, gate, dtype)
+    layouts = _last_runs(g)
+    assert layouts and all(2 <= left < ctas for ctas, left in layouts)
+    first = _pass(g, x, dy, gate, h0, dl)
+    _compare(first, *n, gate, *s, None, dtype == torch.bfloat16)
+    for _ in range(8):
+        for a, b in zip(first, _pass(g, x, dy, gate, h0, dl)):
+            assert np.array_equal(a, b)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    works = [_ws(g) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        outs = []
+        for stream, ws in zip(streams, works):
+            with torch.cuda.stream(stream):
+                outs.append(dastac.linrec_forward(g, x, gate, h0=h0, workspace=ws))
+        torch.cuda.synchronize()
+        for h in outs:
+            assert np.array_equal(first[0], h.float().cpu().double().numpy())
+
+
 @gpu
 @pytest.mark.parametrize("T", [1, 7, 200])
 def test_without_states(T):
