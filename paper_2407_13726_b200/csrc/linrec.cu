@@ -882,9 +882,13 @@ __global__ void __launch_bounds__(kThreads, 2) linrec_forward_kernel(const __gri
             if (ACCESS != kTensor) fetch_tile(it + R, stage);
             continue;
         }
+        if (stop) {   // nothing is written: others may still be composing the maps of the last tile on this side
+            sync_eight(true);
+            break;
+        }
         const int side = it & 1;
         const uint32_t side_turn = it >> 1 & 1;
-        const bool any = !stop && t.any != 0;
+        const bool any = t.any != 0;
         Bounds b{0, 0, 0xffffu, nullptr};
         if (any) b = bounds_of(t, warp);
 
@@ -900,8 +904,8 @@ __global__ void __launch_bounds__(kThreads, 2) linrec_forward_kernel(const __gri
             mbar_arrive(smem_u32(&sm.empty[stage]));
         }
         // with one tile a sequence: read before the last warp writes the state behind it, maybe in the same place
-        if (p.chunks == 1 && warp == 0 && !stop) sm.entering[side][lane] = L::load_state(end_state<false>(p, t), lane, t.live);
-        if (sync_eight(stop)) break;
+        if (p.chunks == 1 && warp == 0) sm.entering[side][lane] = L::load_state(end_state<false>(p, t), lane, t.live);
+        if (sync_eight(false)) break;
 
         bool reset;
         const Map<N> before = compose<N>(sm.A[side], sm.H[side], sm.reset[side], any, 0, warp, 1, lane, reset);

@@ -142,6 +142,25 @@ def test_last_runs_that_lack_tiles_for_some_of_a_cluster(B, groups, tiles, dtype
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("packed", [False, True])
+def test_clusters_that_end_with_a_run_without_a_tile(packed, dtype):
+    """Fewer chains than clusters, a last run that is short: for most CTAs a tile, no tile, and the end follow one another."""
+    D, T, gate = 20 * (64 if dtype == torch.bfloat16 else 32), 128 * 8 + 40, dastac.GATE_SIGMOID
+    off = [0, 300, 301, T - 2] if packed else None
+    (g, x, dy), (h0, dl), n, s = _inputs(41, 1, T, D, gate, dtype, n=3 if packed else 1)
+    layouts = _last_runs(g)
+    assert layouts and all(left < ctas for ctas, left in layouts)
+    offsets = None if off is None else torch.tensor(off, device="cuda")
+    a = (g[0], x[0], dy[0]) if packed else (g, x, dy)
+    first = _pass(*a, gate, h0, dl, offsets)
+    _compare(first, *n, gate, *s, off, dtype == torch.bfloat16)
+    for _ in range(30):
+        for p, q in zip(first, _pass(*a, gate, h0, dl, offsets)):
+            assert np.array_equal(p, q)
+
+
+@gpu
 @pytest.mark.parametrize("T", [1, 7, 200])
 def test_without_states(T):
     (g, x, dy), _, n, _ = _inputs(5, 2, T, 40, dastac.GATE_LOG, torch.float32)
