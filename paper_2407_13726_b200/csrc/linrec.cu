@@ -1298,7 +1298,10 @@ dastac_status run(const dastac_linrec_shape* s, Params& p, void* workspace, size
         p.counter = (unsigned long long*)w;
         p.abort = (uint32_t*)(w + 8);
         p.states = (uint32_t*)(w + 256);
-        if (l.runs > 1 && cudaMemsetAsync(w, 0xff, l.bytes, st) != cudaSuccess) return DASTAC_ERR_CUDA;
+        if (l.runs > 1 && cudaMemsetAsync(w, 0xff, l.bytes, st) != cudaSuccess) {
+            cudaGetLastError();
+            return DASTAC_ERR_CUDA;
+        }
     }
     p.offsets = s->offsets;
     p.sequences = s->sequences;
@@ -1322,10 +1325,13 @@ dastac_status run(const dastac_linrec_shape* s, Params& p, void* workspace, size
 dastac_status no_steps(const dastac_linrec_shape* s, const float* in, int64_t ld_in, float* out, int64_t ld_out, cudaStream_t st) {
     const int64_t rows = s->offsets ? s->sequences : s->batch;
     if (!out || rows == 0 || s->channels == 0 || in == out) return DASTAC_OK;
-    const size_t width = (size_t)s->channels * 4;
-    const cudaError_t e = in ? cudaMemcpy2DAsync(out, (size_t)ld_out * 4, in, (size_t)ld_in * 4, width, (size_t)rows, cudaMemcpyDeviceToDevice, st)
-                             : cudaMemset2DAsync(out, (size_t)ld_out * 4, 0, width, (size_t)rows, st);
-    return e == cudaSuccess ? DASTAC_OK : DASTAC_ERR_CUDA;
+    // a single row may have any pitch, which a copy of rows would refuse
+    const size_t width = (size_t)s->channels * 4, from = rows > 1 ? (size_t)ld_in * 4 : width, to = rows > 1 ? (size_t)ld_out * 4 : width;
+    const cudaError_t e = in ? cudaMemcpy2DAsync(out, to, in, from, width, (size_t)rows, cudaMemcpyDeviceToDevice, st)
+                             : cudaMemset2DAsync(out, to, 0, width, (size_t)rows, st);
+    if (e == cudaSuccess) return DASTAC_OK;
+    cudaGetLastError();
+    return DASTAC_ERR_CUDA;
 }
 
 bool state_ok(const dastac_linrec_shape* s, const float* v, int64_t ld) {

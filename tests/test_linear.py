@@ -260,6 +260,19 @@ def test_backward_empty_extents():
 
 
 @gpu
+def test_backward_empty_extents_and_one_row_of_any_pitch():
+    """A (1, K) tensor made from a column has a pitch of 1, which says nothing for a single row."""
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    dx = torch.ones(16, 1, **bf).t()
+    dastac.linear_backward(torch.ones(1, 0, **bf), torch.ones(1, 16, **bf), torch.ones(0, 16, **bf), dx=dx)
+    assert dx.stride() == (1, 1) and (dx == 0).all()
+    for dw in (torch.ones(16, 1, device="cuda").t(), torch.ones(16, 1, **bf).t()):
+        db = torch.ones(1, device="cuda")
+        dastac.linear_backward(torch.ones(0, 1, **bf), torch.ones(0, 16, **bf), torch.ones(1, 16, **bf), dw=dw, db=db)
+        assert (dw == 0).all() and (db == 0).all()
+
+
+@gpu
 @pytest.mark.parametrize("act", ACTS[1:])
 def test_gradients_against_differences(act):
     """<gradient, direction> against central differences of the 64-bit forward pass.  The kept preactivation is

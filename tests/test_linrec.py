@@ -370,6 +370,24 @@ def test_empty_extents():
             assert torch.equal(last, h0)
 
 
+@gpu
+def test_no_steps_and_one_row_of_any_pitch():
+    """A (1, D) tensor made from a column has a pitch of 1, which says nothing for a single row."""
+    D = 12
+    row = lambda v: torch.full((D, 1), v, device="cuda").t()  # noqa: E731
+    assert row(0.0).stride() == (1, 1)
+    for packed in (False, True):
+        g = torch.zeros((0, D) if packed else (1, 0, D), device="cuda")
+        offsets = torch.zeros(2, dtype=torch.int64, device="cuda") if packed else None
+        last = row(2.0)
+        dastac.linrec_forward(g, g, dastac.GATE_VALUE, h0=row(3.0), h_last=last, offsets=offsets)
+        assert (last == 3).all()
+        dastac.linrec_forward(g, g, dastac.GATE_VALUE, h_last=last, offsets=offsets)
+        assert (last == 0).all()
+        dastac.linrec_backward(g, g, g, dastac.GATE_VALUE, dastac.linrec_empty_carries(g), dh_last=row(4.0), dh0=last, offsets=offsets)
+        assert (last == 4).all()
+
+
 # ---- refusals (no GPU) -------------------------------------------------------------------------------------------
 
 def _shape(**k):
