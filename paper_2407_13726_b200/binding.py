@@ -545,9 +545,21 @@ for _name in ("forward", "backward"):
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _stream_of(t: torch.Tensor) -> int:
-    """The current stream of the tensor's device, without the objects around it."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+def _device_of(t: torch.Tensor) -> int:
+    """The GPU that a call runs on: that of its first tensor.  All its tensors have to lie there."""
+    dev = t.get_device()
+    assert dev >= 0
+    return dev
+
+
+def _launch(call, dev: int, *args) -> int:
+    """``call`` on the current stream of GPU ``dev``, with that GPU current: the library sizes its grids for the current
+    device and launches there."""
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    if torch._C._cuda_getDevice() == dev:
+        return call(*args, stream)
+    with torch.cuda.device(dev):
+        return call(*args, stream)
 
 
 def _code(dtype: torch.dtype) -> int:
@@ -557,7 +569,7 @@ def _code(dtype: torch.dtype) -> int:
     return code
 
 
-def _extents(g: torch.Tensor, offsets: Optional[torch.Tensor]):
+def _extents(g: torch.Tensor, offsets: Optional[torch.Tensor], dev: int):
     """(batch, steps, channels, pointer to the offsets, sequences) of a call."""
     if offsets is None:
         batch, steps, channels = g.shape
@@ -568,14 +580,14 @@ def _extents(g: torch.Tensor, offsets: Optional[torch.Tensor]):
     return 1, steps, channels, offsets.data_ptr(), offsets.numel() - 1
 
 
-def _sequence(t: torch.Tensor, like: torch.Tensor) -> bytes:
+def _sequence(t: torch.Tensor, like: torch.Tensor, dev: int) -> bytes:
     assert t.is_cuda and t.shape == like.shape and t.dtype == like.dtype
     st = t.stride()
     assert st[-1] == 1 or t.shape[-1] <= 1
     return _SEQ.pack(t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
 
 
-def _state(t: Optional[torch.Tensor], rows: int, channels: int):
+def _state(t: Optional[torch.Tensor], rows: int, channels: int, dev: int):
     """Pointer and row pitch of an optional fp32 state tensor, one row a sequence."""
     if t is None:
         return None, 0
@@ -585,12 +597,16 @@ def _state(t: Optional[torch.Tensor], rows: int, channels: int):
     return t.data_ptr(), pitch
 
 
-def _scratch(workspace: Optional[torch.Tensor]):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+def _scratch(workspace: Optional[torch.Tensor], dev: int):
+    if workspace is None:
+        return None, 0
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _pointer(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
+def _error_word(t: Optional[torch.Tensor], dev: int):
+    if t is None:
+        return None
+    return t.data_ptr()
 
 
 @functools.lru_cache(maxsize=1024)
@@ -613,7 +629,7 @@ def linrec_empty_carries(g: torch.Tensor) -> torch.Tensor:
     return torch.empty((batch, -(-steps // LINREC_CHUNK), channels), dtype=torch.float32, device=g.device)
 
 
-def _carries(t: Optional[torch.Tensor], batch: int, steps: int, channels: int):
+def _carries(t: Optional[torch.Tensor], batch: int, steps: int, channels: int, dev: int):
     if t is None:
         return None
     assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous()
@@ -628,16 +644,17 @@ def linrec_forward(g: torch.Tensor, x: torch.Tensor, gate: int, out: Optional[to
     """``h_t = a_t h_{t-1} + u_t`` along the steps of ``g`` and ``x`` (batch x steps x channels; with ``offsets``
     steps x channels, sequences packed behind one another), see ``dastac.h`` for the gates.  ``h_last`` and
     ``carries`` are filled when given; a call with one step is a decoding step."""
-    batch, steps, channels, off, seqs = _extents(g, offsets)
+    dev = _device_of(g)
+    batch, steps, channels, off, seqs = _extents(g, offsets, dev)
     rows = seqs if off else batch
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    p0, ld0 = _state(h0, rows, channels)
-    p1, ld1 = _state(h_last, rows, channels)
-    ws, n = _scratch(workspace)
-    st = _packed.dastac_linrec_forward(_SHAPE.pack(_code(g.dtype), gate, batch, steps, channels, off, seqs), _sequence(g, g),
-                                       _sequence(x, g), p0, ld0, _sequence(out, g), p1, ld1,
-                                       _carries(carries, batch, steps, channels), ws, n, _pointer(err_word), _stream_of(g))
+    p0, ld0 = _state(h0, rows, channels, dev)
+    p1, ld1 = _state(h_last, rows, channels, dev)
+    ws, n = _scratch(workspace, dev)
+    st = _launch(_packed.dastac_linrec_forward, dev, _SHAPE.pack(_code(g.dtype), gate, batch, steps, channels, off, seqs),
+                 _sequence(g, g, dev), _sequence(x, g, dev), p0, ld0, _sequence(out, g, dev), p1, ld1,
+                 _carries(carries, batch, steps, channels, dev), ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linrec_forward")
     return out
@@ -650,25 +667,27 @@ def linrec_backward(g: torch.Tensor, x: torch.Tensor, dy: torch.Tensor, gate: in
                     workspace: Optional[torch.Tensor] = None, err_word: Optional[torch.Tensor] = None):
     """Gradients ``(dg, dx)`` of the recurrence (and ``dh0`` when given) from the gradients ``dy`` of its output
     and ``dh_last`` of its last states; ``carries`` as kept by ``linrec_forward`` on the same inputs."""
-    batch, steps, channels, off, seqs = _extents(g, offsets)
+    dev = _device_of(g)
+    batch, steps, channels, off, seqs = _extents(g, offsets, dev)
     rows = seqs if off else batch
     if dg is None:
         dg = torch.empty_like(g, memory_format=torch.contiguous_format)
     if dx is None:
         dx = torch.empty_like(x, memory_format=torch.contiguous_format)
-    p0, ld0 = _state(h0, rows, channels)
-    p1, ld1 = _state(dh_last, rows, channels)
-    p2, ld2 = _state(dh0, rows, channels)
-    ws, n = _scratch(workspace)
-    st = _packed.dastac_linrec_backward(_SHAPE.pack(_code(g.dtype), gate, batch, steps, channels, off, seqs), _sequence(g, g),
-                                        _sequence(x, g), _sequence(dy, g), p0, ld0, _carries(carries, batch, steps, channels), p1, ld1,
-                                        _sequence(dg, g), _sequence(dx, g), p2, ld2, ws, n, _pointer(err_word), _stream_of(g))
+    p0, ld0 = _state(h0, rows, channels, dev)
+    p1, ld1 = _state(dh_last, rows, channels, dev)
+    p2, ld2 = _state(dh0, rows, channels, dev)
+    ws, n = _scratch(workspace, dev)
+    st = _launch(_packed.dastac_linrec_backward, dev, _SHAPE.pack(_code(g.dtype), gate, batch, steps, channels, off, seqs),
+                 _sequence(g, g, dev), _sequence(x, g, dev), _sequence(dy, g, dev), p0, ld0,
+                 _carries(carries, batch, steps, channels, dev), p1, ld1, _sequence(dg, g, dev), _sequence(dx, g, dev), p2, ld2,
+                 ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linrec_backward")
     return dg, dx
 
 
-def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype=torch.bfloat16):
+def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dev: int, dtype=torch.bfloat16):
     """Pointer and row pitch of an optional rows x cols matrix."""
     if t is None:
         return 0, 0
@@ -678,7 +697,7 @@ def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype=torch.bfloat1
     return t.data_ptr(), pitch
 
 
-def _vector(t: Optional[torch.Tensor], n: int) -> int:
+def _vector(t: Optional[torch.Tensor], n: int, dev: int) -> int:
     if t is None:
         return 0
     assert t.is_cuda and t.dtype == torch.float32 and t.shape == (n,) and (n <= 1 or t.stride(0) == 1)
@@ -690,9 +709,9 @@ _SOMEWHERE = 256   # an aligned address that is not read: workspace queries look
 
 def linear_workspace(x: torch.Tensor, w: torch.Tensor) -> int:
     """Workspace bytes of ``linear_forward`` on these operands (0 when both are aligned)."""
-    (M, K), N = x.shape, w.shape[0]
-    px, ldx = _matrix(x, M, K)
-    pw, ldw = _matrix(w, N, K)
+    (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
+    px, ldx = _matrix(x, M, K, dev)
+    pw, ldw = _matrix(w, N, K, dev)
     if not ((px | pw) & 15 or (ldx | ldw) & 7):
         return 0
     nbytes = ctypes.c_size_t()
@@ -707,14 +726,15 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, y: Optional[torch.Tensor] =
                    workspace: Optional[torch.Tensor] = None, err_word: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``y = f(x w^T + bias) + residual`` for bf16 ``x`` (M x K) and ``w`` (N x K); ``y`` and ``residual`` are bf16 or
     fp32 (bf16 when ``y`` is not given), ``z`` (bf16) receives the preactivation for the backward pass."""
-    (M, K), N = x.shape, w.shape[0]
+    (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
     if y is None:
         y = torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
-    ws, n = _scratch(workspace)
-    st = _packed.dastac_linear_forward(
-        _LINEAR.pack(M, N, K, act, _code(y.dtype), 0, 0, *_matrix(x, M, K), *_matrix(w, N, K), _vector(bias, N),
-                     *_matrix(residual, M, N, y.dtype), *_matrix(y, M, N, y.dtype), *_matrix(z, M, N), 0, 0, 0, 0, 0, 0, 0),
-        ws, n, _pointer(err_word), _stream_of(x))
+    ws, n = _scratch(workspace, dev)
+    st = _launch(
+        _packed.dastac_linear_forward, dev,
+        _LINEAR.pack(M, N, K, act, _code(y.dtype), 0, 0, *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), _vector(bias, N, dev),
+                     *_matrix(residual, M, N, dev, y.dtype), *_matrix(y, M, N, dev, y.dtype), *_matrix(z, M, N, dev), 0, 0, 0, 0, 0, 0, 0),
+        ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linear_forward")
     return y
@@ -722,11 +742,11 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, y: Optional[torch.Tensor] =
 
 def linear_backward_workspace(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int = ACT_NONE) -> int:
     """Workspace bytes of ``linear_backward`` on these operands with every gradient asked for."""
-    (M, K), N = x.shape, w.shape[0]
+    (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
     nbytes = ctypes.c_size_t()
     _check(_packed.dastac_linear_backward_workspace(
-        _LINEAR.pack(M, N, K, act, BF16, BF16, 0, *_matrix(x, M, K), *_matrix(w, N, K), 0, 0, 0, 0, 0, _SOMEWHERE, N,
-                     *_matrix(dy, M, N), _SOMEWHERE, K, _SOMEWHERE, K, _SOMEWHERE), ctypes.byref(nbytes)),
+        _LINEAR.pack(M, N, K, act, BF16, BF16, 0, *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), 0, 0, 0, 0, 0, _SOMEWHERE, N,
+                     *_matrix(dy, M, N, dev), _SOMEWHERE, K, _SOMEWHERE, K, _SOMEWHERE), ctypes.byref(nbytes)),
         "dastac_linear_backward_workspace")
     return int(nbytes.value)
 
@@ -737,12 +757,14 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int
                     err_word: Optional[torch.Tensor] = None) -> None:
     """Fills the gradients that are given: ``dx`` (M x K bf16), ``dw`` (N x K, bf16 or fp32), ``db`` (N fp32);
     ``accumulate`` adds to ``dw`` (fp32) and ``db``."""
-    (M, K), N = x.shape, w.shape[0]
+    (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
     dw_dtype = torch.bfloat16 if dw is None else dw.dtype
-    ws, n = _scratch(workspace)
-    st = _packed.dastac_linear_backward(
-        _LINEAR.pack(M, N, K, act, BF16, _code(dw_dtype), int(accumulate), *_matrix(x, M, K), *_matrix(w, N, K), 0, 0, 0, 0, 0,
-                     *_matrix(z, M, N), *_matrix(dy, M, N), *_matrix(dx, M, K), *_matrix(dw, N, K, dw_dtype), _vector(db, N)),
-        ws, n, _pointer(err_word), _stream_of(x))
+    ws, n = _scratch(workspace, dev)
+    st = _launch(
+        _packed.dastac_linear_backward, dev,
+        _LINEAR.pack(M, N, K, act, BF16, _code(dw_dtype), int(accumulate), *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), 0, 0, 0, 0, 0,
+                     *_matrix(z, M, N, dev), *_matrix(dy, M, N, dev), *_matrix(dx, M, K, dev), *_matrix(dw, N, K, dev, dw_dtype),
+                     _vector(db, N, dev)),
+        ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linear_backward")
