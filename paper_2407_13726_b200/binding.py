@@ -610,17 +610,19 @@ def _error_word(t: Optional[torch.Tensor], dev: int):
 
 
 @functools.lru_cache(maxsize=1024)
-def _linrec_bytes(dtype: torch.dtype, batch: int, steps: int, channels: int) -> int:
+def _linrec_bytes(dev: int, dtype: torch.dtype, batch: int, steps: int, channels: int) -> int:
+    """The size depends on how many multiprocessors the GPU has."""
     nbytes = ctypes.c_size_t()
-    _check(_packed.dastac_linrec_workspace(_SHAPE.pack(_code(dtype), GATE_VALUE, batch, steps, channels, 0, 0), ctypes.byref(nbytes)),
-           "dastac_linrec_workspace")
+    shape = _SHAPE.pack(_code(dtype), GATE_VALUE, batch, steps, channels, 0, 0)
+    with torch.cuda.device(dev):
+        _check(_packed.dastac_linrec_workspace(shape, ctypes.byref(nbytes)), "dastac_linrec_workspace")
     return int(nbytes.value)
 
 
 def linrec_workspace(g: torch.Tensor) -> int:
     """Workspace bytes of the recurrence (either direction) over tensors of the shape and type of ``g``:
     batch x steps x channels, or steps x channels for packed sequences."""
-    return _linrec_bytes(g.dtype, *(g.shape if g.dim() == 3 else (1, *g.shape)))
+    return _linrec_bytes(g.get_device(), g.dtype, *(g.shape if g.dim() == 3 else (1, *g.shape)))
 
 
 def linrec_empty_carries(g: torch.Tensor) -> torch.Tensor:

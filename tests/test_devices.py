@@ -98,3 +98,9 @@ CALLS = [(lambda **k: dastac.linrec_forward(gate=dastac.GATE_LOG, **k), _recurre
 def test_calls_run_on_the_gpu_of_their_tensors(library, call, tensors, dev):
     call(**tensors(dev))
     assert [c[1:] for c in library.calls] == [(dev, 70 + dev)]
+
+
+def test_workspace_of_the_recurrence_is_asked_for_on_each_gpu(library):
+    for dev in (0, 1, 0, 1):
+        assert dastac.linrec_workspace(_Claimed(dev, (2, 900, 8), torch.float32)) == 1000 + dev
+    assert library.calls == [("linrec_workspace", 0, None), ("linrec_workspace", 1, None)]
