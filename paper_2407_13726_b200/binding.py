@@ -575,13 +575,13 @@ def _extents(g: torch.Tensor, offsets: Optional[torch.Tensor], dev: int):
         batch, steps, channels = g.shape
         return batch, steps, channels, 0, 0
     steps, channels = g.shape
-    assert offsets.is_cuda and offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous()
+    assert offsets.get_device() == dev and offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous()
     assert offsets.numel() >= 1
     return 1, steps, channels, offsets.data_ptr(), offsets.numel() - 1
 
 
 def _sequence(t: torch.Tensor, like: torch.Tensor, dev: int) -> bytes:
-    assert t.is_cuda and t.shape == like.shape and t.dtype == like.dtype
+    assert t.get_device() == dev and t.shape == like.shape and t.dtype == like.dtype
     st = t.stride()
     assert st[-1] == 1 or t.shape[-1] <= 1
     return _SEQ.pack(t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
@@ -591,7 +591,7 @@ def _state(t: Optional[torch.Tensor], rows: int, channels: int, dev: int):
     """Pointer and row pitch of an optional fp32 state tensor, one row a sequence."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.dtype == torch.float32 and t.shape == (rows, channels)
+    assert t.get_device() == dev and t.dtype == torch.float32 and t.shape == (rows, channels)
     pitch, unit = t.stride()
     assert unit == 1 or channels <= 1
     return t.data_ptr(), pitch
@@ -600,12 +600,14 @@ def _state(t: Optional[torch.Tensor], rows: int, channels: int, dev: int):
 def _scratch(workspace: Optional[torch.Tensor], dev: int):
     if workspace is None:
         return None, 0
+    assert workspace.get_device() == dev and workspace.is_contiguous()
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _error_word(t: Optional[torch.Tensor], dev: int):
     if t is None:
         return None
+    assert t.get_device() == dev and t.dtype == torch.int32 and t.numel() >= 1
     return t.data_ptr()
 
 
@@ -634,7 +636,7 @@ def linrec_empty_carries(g: torch.Tensor) -> torch.Tensor:
 def _carries(t: Optional[torch.Tensor], batch: int, steps: int, channels: int, dev: int):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous()
+    assert t.get_device() == dev and t.dtype == torch.float32 and t.is_contiguous()
     assert t.shape == (batch, -(-steps // LINREC_CHUNK), channels)
     return t.data_ptr()
 
@@ -693,7 +695,7 @@ def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dev: int, dtype=tor
     """Pointer and row pitch of an optional rows x cols matrix."""
     if t is None:
         return 0, 0
-    assert t.is_cuda and t.dtype == dtype and t.shape == (rows, cols)
+    assert t.get_device() == dev and t.dtype == dtype and t.shape == (rows, cols)
     pitch, unit = t.stride()
     assert unit == 1 or cols <= 1
     return t.data_ptr(), pitch
@@ -702,7 +704,7 @@ def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dev: int, dtype=tor
 def _vector(t: Optional[torch.Tensor], n: int, dev: int) -> int:
     if t is None:
         return 0
-    assert t.is_cuda and t.dtype == torch.float32 and t.shape == (n,) and (n <= 1 or t.stride(0) == 1)
+    assert t.get_device() == dev and t.dtype == torch.float32 and t.shape == (n,) and (n <= 1 or t.stride(0) == 1)
     return t.data_ptr()
 
 

@@ -100,6 +100,22 @@ def test_calls_run_on_the_gpu_of_their_tensors(library, call, tensors, dev):
     assert [c[1:] for c in library.calls] == [(dev, 70 + dev)]
 
 
+@pytest.mark.parametrize("call,tensors", CALLS)
+def test_tensors_of_another_gpu_or_of_the_host_are_refused(library, call, tensors):
+    names = list(tensors(1))
+    for name in names:
+        for other in (0, -1):
+            k = tensors(1)
+            k[name] = _Claimed(other, tuple(k[name].shape), k[name].dtype) if other == 0 else k[name]._t
+            with pytest.raises(AssertionError):
+                call(**k)
+    k = tensors(1)
+    k["workspace"]._t = torch.empty(128, dtype=torch.uint8)[::2]   # its bytes do not lie behind one another
+    with pytest.raises(AssertionError):
+        call(**k)
+    assert not library.calls
+
+
 def test_workspace_of_the_recurrence_is_asked_for_on_each_gpu(library):
     for dev in (0, 1, 0, 1):
         assert dastac.linrec_workspace(_Claimed(dev, (2, 900, 8), torch.float32)) == 1000 + dev
