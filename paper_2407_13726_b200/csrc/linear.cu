@@ -14,9 +14,11 @@
 // instruction is wasted, and the contraction is split over the CTAs of a cluster, which join their partial
 // sums through distributed shared memory in a fixed order.
 //
-// Precision: a sum in the tensor core's fp32 accumulator loses more than sums rounded to nearest would; over 1000 terms
-// its error was 1.1e-6 of the result.  Where the result is fp32 and tensor memory has room, two accumulators take the
-// blocks of k in turn and are added at the end: 5.3e-7, at the same time.  Results in bf16 are rounded far above either.
+// Precision: the tensor core's fp32 accumulator loses what a sum rounded to nearest would not, always towards zero, and
+// the more the longer the sum: 1.0e-6 of the result over 1000 terms, 4.4e-6 over 4096, 9.1e-6 over 8192.  Where the result
+// is fp32, an accumulator therefore takes a few blocks of k and is then folded: the epilogue's warps add it to a sum in
+// their registers, rounded to nearest, while the tensor cores fill the other one.  4.6e-7 to 6.5e-7 at any length, for 11 %
+// of the time (4096 x 4096 x 4096, fp32: 108 us, 97 in one accumulator).  Results in bf16 are rounded far above either.
 //
 // Every wait on an mbarrier is bounded by a clock budget; on expiry the error word is set and the CTA drains.
 #include <cuda.h>
@@ -30,6 +32,14 @@ namespace dastac {
 namespace {
 
 constexpr int kBlockK = 64;
+constexpr int kFoldBlocks = 8;
+// Blocks of k that an accumulator takes, with `left` of `all` to go.  The first one of a long contraction takes twice as many:
+// the tensor cores work on it while the epilogue of the tile before still holds the other (4096 x 4096 x 4096, fp32: 108 us,
+// 113 with equal parts).
+__device__ __forceinline__ int fold_blocks(int left, int all) {
+    const int most = left == all && all >= 4 * kFoldBlocks ? 2 * kFoldBlocks : kFoldBlocks;
+    return left < most ? left : most;
+}
 enum ErrCode : int32_t { kErrFull = 0x4c01, kErrEmpty = 0x4c03, kErrTmemFull = 0x4c04, kErrTmemEmpty = 0x4c05 };
 
 // ---- activations -------------------------------------------------------------------------------------
@@ -82,7 +92,7 @@ struct Problem {
     int32_t a_mn, b_mn;                      // the operand's row index is the contiguous one
     int32_t k_blocks, row_blocks, col_blocks;  // blocks of 64, 256 and 256
     int32_t act, out_dtype, accumulate;
-    int32_t split;    // two accumulators take the blocks of k in turn
+    int32_t fold;     // pairs: accumulators are added to sums in registers every few blocks of k
     int32_t even, quad, whole, wide;   // out, z and residual take 2 columns, 4 columns, 16 bytes, 32 bytes in an aligned access
     int64_t rows, cols;
     void* out;
@@ -135,6 +145,25 @@ __device__ __forceinline__ bool peek(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // The MMA and its commit by one elected lane of a converged warp: descriptors stay in uniform registers, which a branch
 // on the lane would take away.
@@ -319,12 +348,6 @@ __device__ __forceinline__ void pair_epilogue(const Problem& q, uint32_t taddr, 
             tmem_ld_wait();
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = q.k_blocks ? __uint_as_float(w[j]) : 0.f;
-            if (q.split) {
-                tmem_ld32(taddr + 256 + 32 * cc, w);
-                tmem_ld_wait();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
-            }
         }
         if (q.bias) {   // the same word for all lanes
             if (n == 32 && ((uintptr_t)q.bias & 15) == 0) {
@@ -378,7 +401,7 @@ __device__ __forceinline__ void pair_epilogue(const Problem& q, uint32_t taddr, 
     }
 }
 
-template <bool DIRECT>
+template <bool DIRECT, bool FOLD>   // FOLD: some problem asks for it
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap b0,
                    const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b1, const __grid_constant__ PairParams p) {
@@ -492,10 +515,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
     } else if (warp == kWarpMma) {
         if (rank == 0) {
             Turn turn{0, 0};
-            uint32_t tile_n = 0;
+            uint32_t pass_n = 0;
             bool ok = true;
             const uint64_t a_k = operand(smem_base, false), a_m = operand(smem_base, true);
-            auto multiply_tile = [&](uint32_t d_tmem, uint64_t a, uint64_t b, uint64_t a_next, uint64_t b_next, uint32_t idesc, int k_blocks, int split) {
+            auto multiply_tile = [&](uint32_t d_tmem, uint64_t a, uint64_t b, uint64_t a_next, uint64_t b_next, uint32_t idesc, int k_blocks) {
                 bool ready = false;
                 for (int kb = 0; kb < k_blocks; ++kb) {
                     if (!__all_sync(~0u, ready || wait_stage(full(turn.s), turn.parity, abort_flag, p.err_word, kErrFull))) return false;
@@ -506,7 +529,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
                     ready = kb + 1 < k_blocks && peek(full(turn.s), turn.parity);
 #pragma unroll
                     for (int k16 = 0; k16 < kBlockK / 16; ++k16)
-                        umma_elected_pair(d_tmem + (kb & split) * 256, a + at + k16 * a_next, b + at + k16 * b_next, idesc, (kb > split || k16 > 0) ? 1u : 0u);
+                        umma_elected_pair(d_tmem, a + at + k16 * a_next, b + at + k16 * b_next, idesc, (kb > 0 || k16 > 0) ? 1u : 0u);
                     commit_elected_pair(release);
                 }
                 return true;
@@ -517,18 +540,22 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
                 int which, R, C;
                 locate(t, which, R, C);
                 const Problem& q = p.q[which];
-                const int acc = tile_n & 1;
-                const uint32_t use = tile_n >> 1;
-                if (use >= 1 && !__all_sync(~0u, wait_stage(tmem_empty(acc), (use - 1) & 1, abort_flag, p.err_word, kErrTmemEmpty))) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
                 const uint64_t b0d = (q.b_mn ? a_m : a_k) + (kOperandBytes >> 4);
-                ok = multiply_tile(tmem_base + acc * 256, q.a_mn ? a_m : a_k, b0d, q.a_mn ? kNextMn : kNextK, q.b_mn ? kNextMn : kNextK,
-                                   instruction(256, 256, q.a_mn, q.b_mn), q.k_blocks, q.split);
-                if (ok) commit_elected_pair(tmem_full(acc));
-                ++tile_n;
+                int left = q.k_blocks;
+                do {   // an accumulator at a time: all of the contraction, or a few blocks of it
+                    const int acc = pass_n & 1, blocks = FOLD && q.fold ? fold_blocks(left, q.k_blocks) : left;
+                    const uint32_t use = pass_n >> 1;
+                    if (use >= 1 && !__all_sync(~0u, wait_stage(tmem_empty(acc), (use - 1) & 1, abort_flag, p.err_word, kErrTmemEmpty))) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    ok = multiply_tile(tmem_base + acc * 256, q.a_mn ? a_m : a_k, b0d, q.a_mn ? kNextMn : kNextK, q.b_mn ? kNextMn : kNextK,
+                                       instruction(256, 256, q.a_mn, q.b_mn), blocks);
+                    if (ok) commit_elected_pair(tmem_full(acc));
+                    ++pass_n;
+                    left -= blocks;
+                } while (ok && left > 0);
             }
             if (!ok) {
                 commit_elected_pair(drain_bar);
@@ -541,7 +568,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
         const uint32_t empty0 = map_to_cta(tmem_empty(0), 0);
         const int quarter = warp & 3, half = warp >> 2;
         float* const stage = (float*)(epi + warp * kEpiBytes);
-        uint32_t tile_n = 0;
+        uint32_t pass_n = 0;
         bool ok = true;
         for (uint32_t n = 0; n < rounds && ok; ++n) {
             const int64_t t = tile_of(n);
@@ -549,14 +576,55 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
             int which, R, C;
             locate(t, which, R, C);
             const Problem& q = p.q[which];
-            const int acc = tile_n & 1;
-            if (!mbar_wait_warp(tmem_full(acc), (tile_n >> 1) & 1, abort_flag, p.err_word, kErrTmemFull, lane)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * 256 + half * 128;
+            uint32_t taddr;
+            auto wait_accumulator = [&]() {
+                const int acc = pass_n & 1;
+                if (!mbar_wait_warp(tmem_full(acc), (pass_n >> 1) & 1, abort_flag, p.err_word, kErrTmemFull, lane)) return false;
+                tc_fence_after();
+                taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * 256 + half * 128;
+                return true;
+            };
+            auto free_accumulator = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(empty0 + 8u * (pass_n & 1));
+                ++pass_n;
+            };
+            ok = wait_accumulator();
+            if (!ok) break;
             const int64_t row0 = (int64_t)R * 256 + rank * 128 + quarter * 32, col0 = (int64_t)C * 256 + half * 128;
+            if (FOLD && q.fold) {   // the accumulators in turn, their sum back into the last one
+                float sum[8][16];
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] = 0.f;
+                int left = q.k_blocks;
+                while (true) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t w[16];
+                        tmem_ld16(taddr + 16 * c, w);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[c][j] += __uint_as_float(w[j]);
+                    }
+                    left -= fold_blocks(left, q.k_blocks);
+                    if (left == 0) break;
+                    free_accumulator();
+                    ok = wait_accumulator();
+                    if (!ok) break;
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(sum[c][j]);
+                    tmem_st16(taddr + 16 * c, w);
+                }
+                tmem_st_wait();
+            }
             if (row0 < q.rows) switch (q.act) {
                 case DASTAC_ACT_RELU: pair_epilogue<DASTAC_ACT_RELU, DIRECT>(q, taddr, stage, row0, col0, lane); break;
                 case DASTAC_ACT_SIGMOID: pair_epilogue<DASTAC_ACT_SIGMOID, DIRECT>(q, taddr, stage, row0, col0, lane); break;
@@ -564,10 +632,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
                 case DASTAC_ACT_GELU: pair_epilogue<DASTAC_ACT_GELU, DIRECT>(q, taddr, stage, row0, col0, lane); break;
                 default: pair_epilogue<DASTAC_ACT_NONE, DIRECT>(q, taddr, stage, row0, col0, lane); break;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(empty0 + 8u * acc);
-            ++tile_n;
+            free_accumulator();
         }
     }
     // Neither CTA may leave, or give back tensor memory, while its peer can still touch it.
@@ -624,15 +689,6 @@ __device__ __forceinline__ void commit_elected_one(uint32_t bar) {
         "{\n\t.reg .pred e;\n\t"
         "elect.sync _|e, 0xffffffff;\n\t"
         "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
         : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
@@ -724,6 +780,11 @@ __device__ __forceinline__ void slim_finish(const Problem& q, const float* part,
     }
 }
 
+// How a CTA's sum is kept: in one accumulator; in two that take the blocks of k in turn and are added at the end (fp32
+// results, up to 2 kFoldBlocks blocks of k); folded (fp32 results, more blocks).  1 x 4096 x 4096, 16 blocks a CTA: 8.3 us in two
+// accumulators, 8.9 folded; 128 x 19000 x 8192, 128 blocks: 87.8 us folded, 85.4 in two with three times the error.
+enum Sums { kOneSum, kTwoSums, kFolded };
+template <Sums SUMS>
 __global__ void __launch_bounds__(kSlimThreads, 1)
 linear_slim_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant__ CUtensorMap mx, const __grid_constant__ SlimParams p) {
     extern __shared__ uint8_t smem_raw[];
@@ -739,13 +800,14 @@ linear_slim_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int s) { return bar0 + 8u * s; };
     auto empty = [&](int s) { return bar0 + 8u * (stages + s); };
-    const uint32_t done = bar0 + 8u * (2 * stages);
-    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * stages + 1);
+    auto tmem_full = [&](uint32_t a) { return bar0 + 8u * (2 * stages + a); };
+    auto tmem_empty = [&](uint32_t a) { return bar0 + 8u * (2 * stages + 2 + a); };
+    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * stages + 4);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t smem_base = smem_u32(smem);
     const int each = tokens < 32 ? 32 : tokens;   // columns of an accumulator
-    const uint32_t tmem_cols = each << p.q.split;
+    const uint32_t tmem_cols = SUMS == kOneSum ? each : 2 * each;
 
     if (warp == kSlimTma && lane == 0) {
         prefetch_map(&mw);
@@ -756,7 +818,10 @@ linear_slim_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
-        mbar_init(done, 1);
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tmem_full(a), 1);
+            mbar_init(tmem_empty(a), kSlimEpi);
+        }
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -807,9 +872,19 @@ linear_slim_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant
         const uint32_t idesc = instruction(128, tokens, q.b_mn, q.a_mn);
         const uint64_t w0 = operand(smem_base, q.b_mn), x0 = operand(smem_base + kOperandBytes, q.a_mn);
         const uint64_t w_next = q.b_mn ? kNextMn : kNextK, x_next = q.a_mn ? kNextMn : kNextK;
-        const int split = q.split;
+        uint32_t d = tmem_base, pass_n = 0;
+        int begin = k_begin, end = SUMS == kFolded && k_end - k_begin > kFoldBlocks ? k_begin + kFoldBlocks : k_end;
         bool ready = false;
         for (int kb = k_begin; kb < k_end; ++kb) {
+            if (SUMS == kFolded && kb == end) {   // the next accumulator, as in the kernel on pairs
+                commit_elected_one(tmem_full(pass_n & 1));
+                ++pass_n;
+                const uint32_t acc = pass_n & 1, use = pass_n >> 1;
+                if (use > 0 && !__all_sync(~0u, wait_stage(tmem_empty(acc), (use - 1) & 1, abort_flag, p.err_word, kErrTmemEmpty))) break;
+                d = tmem_base + acc * each;
+                begin = kb;
+                end = k_end - kb > kFoldBlocks ? kb + kFoldBlocks : k_end;
+            }
             if (!__all_sync(~0u, ready || wait_stage(full(turn.s), turn.parity, abort_flag, p.err_word, kErrFull))) break;
             tc_fence_after();
             const uint64_t at = (uint64_t)(turn.s * (stage_bytes >> 4));
@@ -818,49 +893,90 @@ linear_slim_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant
             ready = kb + 1 < k_end && peek(full(turn.s), turn.parity);
 #pragma unroll
             for (int k16 = 0; k16 < kBlockK / 16; ++k16)
-                umma_elected_one(tmem_base + ((kb - k_begin) & split) * each, w0 + at + k16 * w_next, x0 + at + k16 * x_next, idesc,
-                                 (kb > k_begin + split || k16 > 0) ? 1u : 0u);
+                umma_elected_one(SUMS == kTwoSums ? d + ((kb - begin) & 1) * each : d, w0 + at + k16 * w_next, x0 + at + k16 * x_next, idesc,
+                                 (kb > begin + (SUMS == kTwoSums) || k16 > 0) ? 1u : 0u);
             commit_elected_one(release);
         }
-        commit_elected_one(done);
-    } else {
-        mbar_wait_warp(done, 0, abort_flag, p.err_word, kErrTmemFull, lane);
-        tc_fence_after();
+        commit_elected_one(tmem_full(pass_n & 1));
     }
     __syncwarp();
+    // Epilogue warp w: lanes 32 (w mod 4) .., the first or the second half of the columns
+    const int half = tokens < 32 ? 16 : tokens / 2, first = (warp >> 2) * half;
+    const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + first;
+    float sum[SUMS == kFolded ? 4 : 1][16];
+    if (warp < kSlimEpi) {
+        mbar_wait_warp(tmem_full(0), 0, abort_flag, p.err_word, kErrTmemFull, lane);
+        tc_fence_after();
+        if constexpr (SUMS == kFolded) {   // the accumulators in turn
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[c][j] = 0.f;
+            uint32_t pass_n = 0;
+            for (int left = k_end - k_begin;;) {
+                const uint32_t acc = pass_n & 1;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (16 * c >= half || first >= tokens) break;   // the same for the whole warp
+                    uint32_t w[16];
+                    tmem_ld16(taddr + acc * each + 16 * c, w);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] += __uint_as_float(w[j]);
+                }
+                left -= kFoldBlocks;
+                if (left <= 0) break;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(tmem_empty(acc));
+                ++pass_n;
+                if (!mbar_wait_warp(tmem_full(pass_n & 1), pass_n >> 1 & 1, abort_flag, p.err_word, kErrTmemFull, lane)) break;
+                tc_fence_after();
+            }
+        }
+    }
     // every CTA of the cluster has started: its shared memory may be written
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (warp < kSlimEpi) {   // warp w: lanes 32 (w mod 4) .., the first or the second half of the columns
-        const int half = tokens < 32 ? 16 : tokens / 2, first = (warp >> 2) * half;
+    if (warp < kSlimEpi) {
         const int end = (int)min((int64_t)min(tokens, first + half), q.rows - m0);   // columns behind the last token are not sent
-        const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
         const int row = (warp & 3) * 32 + lane;
         const bool any = k_end > k_begin;
         const uint32_t part0 = smem_u32(part) + 4u * (rank * most * 128 + row);
         uint32_t owner = first % ranks, i = first / ranks;
-        for (int c0 = first; c0 < end; c0 += 16) {
-            uint32_t v[16];
-            tmem_ld16(taddr + c0, v);
-            tmem_ld_wait();
-            if (q.split && k_end > k_begin + 1) {
-                uint32_t w[16];
-                tmem_ld16(taddr + each + c0, w);
-                tmem_ld_wait();
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(w[j]));
-            }
+        auto send = [&](int c0, const float (&v)[16]) {
             if (ranks == 1) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) part[(c0 + j) * 128 + row] = any ? __uint_as_float(v[j]) : 0.f;
+                for (int j = 0; j < 16; ++j) part[(c0 + j) * 128 + row] = any ? v[j] : 0.f;
             } else {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    if (c0 + j < end) st_cluster(map_to_cta(part0 + 512u * i, owner), any ? __uint_as_float(v[j]) : 0.f);
+                    if (c0 + j < end) st_cluster(map_to_cta(part0 + 512u * i, owner), any ? v[j] : 0.f);
                     if (++owner == ranks) {
                         owner = 0;
                         ++i;
                     }
                 }
+            }
+        };
+        if constexpr (SUMS == kFolded) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (first + 16 * c < end) send(first + 16 * c, sum[c]);
+        } else {
+            for (int c0 = first; c0 < end; c0 += 16) {
+                uint32_t w[16];
+                tmem_ld16(taddr + c0 - first, w);
+                tmem_ld_wait();
+                float v[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]);
+                if (SUMS == kTwoSums && k_end > k_begin + 1) {
+                    tmem_ld16(taddr + each + c0 - first, w);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j] += __uint_as_float(w[j]);
+                }
+                send(c0, v);
             }
         }
         tc_fence_before();
@@ -1127,13 +1243,13 @@ bool set_smem_once(const void* kernel, size_t bytes, bool* done) {
     return true;
 }
 
-template <bool DIRECT>
+template <bool DIRECT, bool FOLD>
 dastac_status launch_pair_as(const PairParams& p, const Maps& m0, const Maps& m1, cudaStream_t st) {
     static bool attr[64];
-    if (!set_smem_once((const void*)linear_pair_kernel<DIRECT>, kPairSmem<DIRECT>, attr)) return DASTAC_ERR_CUDA;
+    if (!set_smem_once((const void*)linear_pair_kernel<DIRECT, FOLD>, kPairSmem<DIRECT>, attr)) return DASTAC_ERR_CUDA;
     const int64_t most = sm_count() / 2;
     const int clusters = (int)(p.tiles < most ? p.tiles : most);
-    linear_pair_kernel<DIRECT><<<2 * clusters, kPairThreads, kPairSmem<DIRECT>, st>>>(m0.a, m0.b, m1.a, m1.b, p);
+    linear_pair_kernel<DIRECT, FOLD><<<2 * clusters, kPairThreads, kPairSmem<DIRECT>, st>>>(m0.a, m0.b, m1.a, m1.b, p);
     return launch_status();
 }
 dastac_status launch_pair(const Problem* q, const Maps* m, int n, int32_t* err_word, cudaStream_t st) {
@@ -1143,10 +1259,11 @@ dastac_status launch_pair(const Problem* q, const Maps* m, int n, int32_t* err_w
     p.tiles0 = tiles_of(q[0]);
     p.tiles = p.tiles0 + (n > 1 ? tiles_of(q[1]) : 0);
     p.err_word = err_word;
-    // with one tile a cluster the accumulator of its next tile is free
-    if (p.tiles <= sm_count() / 2)
-        for (int i = 0; i < 2; ++i) p.q[i].split = p.q[i].out_dtype == DASTAC_F32 && p.q[i].k_blocks > 1;
-    return q[0].whole && q[n - 1].whole ? launch_pair_as<true>(p, m[0], m[n - 1], st) : launch_pair_as<false>(p, m[0], m[n - 1], st);
+    for (Problem& one : p.q) one.fold = one.out_dtype == DASTAC_F32 && one.k_blocks > kFoldBlocks;
+    const bool direct = q[0].whole && q[n - 1].whole;
+    if (p.q[0].fold || p.q[1].fold)
+        return direct ? launch_pair_as<true, true>(p, m[0], m[n - 1], st) : launch_pair_as<false, true>(p, m[0], m[n - 1], st);
+    return direct ? launch_pair_as<true, false>(p, m[0], m[n - 1], st) : launch_pair_as<false, false>(p, m[0], m[n - 1], st);
 }
 
 // CTAs of the slim kernel that the device holds at once in clusters of `ranks`, `per_sm` on a multiprocessor: clusters have
@@ -1169,7 +1286,7 @@ int64_t slim_slots(int dev, int sms, int ranks, int per_sm) {
         cfg.attrs = at;
         cfg.numAttrs = 1;
         int clusters = 0;
-        if (cudaOccupancyMaxActiveClusters(&clusters, linear_slim_kernel, &cfg) != cudaSuccess || clusters <= 0) {
+        if (cudaOccupancyMaxActiveClusters(&clusters, linear_slim_kernel<kOneSum>, &cfg) != cudaSuccess || clusters <= 0) {
             cudaGetLastError();
             return guess;
         }
@@ -1210,9 +1327,11 @@ SlimPlan lay_out_slim(const Problem& q, int dev, int sms, int tokens, int ranks)
 }
 SlimPlan plan_slim(const Problem& q) {
     SlimPlan best{0, 1, 1, 0, 1e30};
-    static bool attr[64];
+    static bool attr[3][64];
     int dev = 0;
-    if (!set_smem_once((const void*)linear_slim_kernel, kSlimMax + 2048, attr) || cudaGetDevice(&dev) != cudaSuccess) return best;
+    if (!set_smem_once((const void*)linear_slim_kernel<kOneSum>, kSlimMax + 2048, attr[kOneSum]) ||
+        !set_smem_once((const void*)linear_slim_kernel<kTwoSums>, kSlimMax + 2048, attr[kTwoSums]) ||
+        !set_smem_once((const void*)linear_slim_kernel<kFolded>, kSlimMax + 2048, attr[kFolded]) || cudaGetDevice(&dev) != cudaSuccess) return best;
     const int sms = sm_count();
     const int least = q.a_mn ? 64 : 16;
     for (int t = least; t <= 128; t *= 2) {
@@ -1248,7 +1367,6 @@ dastac_status launch_slim(const SlimPlan& plan, const Problem& q, const Operand&
     const int ranks = plan.ranks;
     SlimParams p{};
     p.q = q;
-    p.q.split = q.out_dtype == DASTAC_F32;
     p.tokens = plan.tokens;
     p.stages = plan.stages;
     p.err_word = err_word;
@@ -1268,7 +1386,9 @@ dastac_status launch_slim(const SlimPlan& plan, const Problem& q, const Operand&
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, linear_slim_kernel, mw, mx, p) != cudaSuccess) {
+    const bool few = q.out_dtype != DASTAC_F32 || q.k_blocks <= 1, folded = q.k_blocks > 2 * kFoldBlocks * ranks;   // some CTA has more blocks than two accumulators take
+    auto kernel = few ? linear_slim_kernel<kOneSum> : folded ? linear_slim_kernel<kFolded> : linear_slim_kernel<kTwoSums>;
+    if (cudaLaunchKernelEx(&cfg, kernel, mw, mx, p) != cudaSuccess) {
         cudaGetLastError();
         return DASTAC_ERR_CUDA;
     }

@@ -272,6 +272,28 @@ def test_backward_empty_extents_and_one_row_of_any_pitch():
         assert (dw == 0).all() and (db == 0).all()
 
 
+# An fp32 result is a sum of parts, each of at most 64 sums of 16 products that join an accumulator one after the other.
+# The accumulator is cut off rather than rounded: half an ulp (2^-24) each in the mean, of a sum that grows with the root of
+# the number of terms, 2/3 of its final size in the mean.  The parts and what follows are rounded to nearest.
+FOLDED = 64 * 2 / 3 * 2.0 ** -24 + 2.0 ** -22
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(600, 600, 8192), (2600, 2600, 8192), (2600, 2600, 2100), (2600, 130, 16384), (100, 19000, 8192), (1, 5000, 8192)])
+def test_fp32_results_of_long_sums(M, N, K):
+    """The same accuracy for many tiles as for few, and for any length."""
+    gen = torch.Generator().manual_seed(M + N)
+    x, w = _rand(gen, M, K), _rand(gen, N, K)
+    y = dastac.linear_forward(x, w, torch.empty(M, N, device="cuda"), workspace=_ws(dastac.linear_workspace(x, w)))
+    ref = x.double() @ w.double().T
+    assert float((y - ref).norm()) <= FOLDED * float(ref.norm())
+    dy, xs, dw = _rand(gen, K, M), _rand(gen, K, N), torch.empty(M, N, device="cuda")   # the sum is over the K rows here
+    unused = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    dastac.linear_backward(dy, xs, unused, dw=dw, workspace=_ws(dastac.linear_backward_workspace(dy, xs, unused)))
+    ref = dy.double().T @ xs.double()
+    assert float((dw - ref).norm()) <= FOLDED * float(ref.norm())
+
+
 @gpu
 @pytest.mark.parametrize("act", ACTS[1:])
 def test_gradients_against_differences(act):
