@@ -515,11 +515,12 @@ class _LinearArgs(ctypes.Structure):
                 ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
                 ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64), ("z", ctypes.c_void_p), ("ldz", ctypes.c_int64),
                 ("dy", ctypes.c_void_p), ("lddy", ctypes.c_int64), ("dx", ctypes.c_void_p), ("lddx", ctypes.c_int64),
-                ("dw", ctypes.c_void_p), ("lddw", ctypes.c_int64), ("db", ctypes.c_void_p)]
+                ("dw", ctypes.c_void_p), ("lddw", ctypes.c_int64), ("db", ctypes.c_void_p),
+                ("round_dz", ctypes.c_int32)]
 
 
 # the same layouts for struct.pack
-_SHAPE, _SEQ, _LINEAR = struct.Struct("@iiqqqPq"), struct.Struct("@Pqq"), struct.Struct("@qqqiiiiPqPqPPqPqPqPqPqPqP")
+_SHAPE, _SEQ, _LINEAR = struct.Struct("@iiqqqPq"), struct.Struct("@Pqq"), struct.Struct("@qqqiiiiPqPqPPqPqPqPqPqPqPi0P")
 assert (_SHAPE.size, _SEQ.size, _LINEAR.size) == tuple(map(ctypes.sizeof, (_LinrecShape, _Sequence, _LinearArgs)))
 
 _shape_p, _seq_p, _linear_p = ctypes.POINTER(_LinrecShape), ctypes.POINTER(_Sequence), ctypes.POINTER(_LinearArgs)
@@ -720,7 +721,7 @@ def linear_workspace(x: torch.Tensor, w: torch.Tensor) -> int:
         return 0
     nbytes = ctypes.c_size_t()
     _check(_packed.dastac_linear_forward_workspace(
-        _LINEAR.pack(M, N, K, 0, BF16, 0, 0, px, ldx, pw, ldw, 0, 0, 0, _SOMEWHERE, N, *[0] * 9), ctypes.byref(nbytes)),
+        _LINEAR.pack(M, N, K, 0, BF16, 0, 0, px, ldx, pw, ldw, 0, 0, 0, _SOMEWHERE, N, *[0] * 10), ctypes.byref(nbytes)),
         "dastac_linear_forward_workspace")
     return int(nbytes.value)
 
@@ -737,20 +738,22 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, y: Optional[torch.Tensor] =
     st = _launch(
         _packed.dastac_linear_forward, dev,
         _LINEAR.pack(M, N, K, act, _code(y.dtype), 0, 0, *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), _vector(bias, N, dev),
-                     *_matrix(residual, M, N, dev, y.dtype), *_matrix(y, M, N, dev, y.dtype), *_matrix(z, M, N, dev), 0, 0, 0, 0, 0, 0, 0),
+                     *_matrix(residual, M, N, dev, y.dtype), *_matrix(y, M, N, dev, y.dtype), *_matrix(z, M, N, dev), 0, 0, 0, 0, 0, 0, 0, 0),
         ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linear_forward")
     return y
 
 
-def linear_backward_workspace(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int = ACT_NONE) -> int:
-    """Workspace bytes of ``linear_backward`` on these operands with every gradient asked for."""
+def linear_backward_workspace(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int = ACT_NONE,
+                              dw_dtype: torch.dtype = torch.float32, round_dz: bool = False) -> int:
+    """Workspace bytes of ``linear_backward`` on these operands with every gradient asked for.  With an activation an fp32
+    ``dw`` takes more than a bf16 one or one with ``round_dz``; what the defaults give is enough for each."""
     (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
     nbytes = ctypes.c_size_t()
     _check(_packed.dastac_linear_backward_workspace(
-        _LINEAR.pack(M, N, K, act, BF16, BF16, 0, *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), 0, 0, 0, 0, 0, _SOMEWHERE, N,
-                     *_matrix(dy, M, N, dev), _SOMEWHERE, K, _SOMEWHERE, K, _SOMEWHERE), ctypes.byref(nbytes)),
+        _LINEAR.pack(M, N, K, act, BF16, _code(dw_dtype), 0, *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), 0, 0, 0, 0, 0, _SOMEWHERE, N,
+                     *_matrix(dy, M, N, dev), _SOMEWHERE, K, _SOMEWHERE, K, _SOMEWHERE, int(round_dz)), ctypes.byref(nbytes)),
         "dastac_linear_backward_workspace")
     return int(nbytes.value)
 
@@ -758,9 +761,10 @@ def linear_backward_workspace(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor
 def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int = ACT_NONE, z: Optional[torch.Tensor] = None,
                     dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None,
                     accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
-                    err_word: Optional[torch.Tensor] = None) -> None:
+                    err_word: Optional[torch.Tensor] = None, round_dz: bool = False) -> None:
     """Fills the gradients that are given: ``dx`` (M x K bf16), ``dw`` (N x K, bf16 or fp32), ``db`` (N fp32);
-    ``accumulate`` adds to ``dw`` (fp32) and ``db``."""
+    ``accumulate`` adds to ``dw`` (fp32) and ``db``.  With an activation an fp32 ``dw`` takes two products, for the two
+    bf16 parts of dZ; ``round_dz`` leaves the second one out."""
     (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
     dw_dtype = torch.bfloat16 if dw is None else dw.dtype
     ws, n = _scratch(workspace, dev)
@@ -768,7 +772,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int
         _packed.dastac_linear_backward, dev,
         _LINEAR.pack(M, N, K, act, BF16, _code(dw_dtype), int(accumulate), *_matrix(x, M, K, dev), *_matrix(w, N, K, dev), 0, 0, 0, 0, 0,
                      *_matrix(z, M, N, dev), *_matrix(dy, M, N, dev), *_matrix(dx, M, K, dev), *_matrix(dw, N, K, dev, dw_dtype),
-                     _vector(db, N, dev)),
+                     _vector(db, N, dev), int(round_dz)),
         ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linear_backward")

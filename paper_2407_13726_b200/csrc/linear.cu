@@ -1014,8 +1014,8 @@ __global__ void linear_repitch_kernel(const uint16_t* __restrict__ src, int64_t 
     }
 }
 
-// dZ = dY f'(Z), rounded to bf16 for the products, and the column sums of the unrounded values over 64 rows;
-// VEC = 8: rows of whole aligned 16-byte words.  Bound by memory: a warp has four rows in flight.  The sums of the row
+// dZ = dY f'(Z), rounded to bf16 for the products, where asked for also what that rounding leaves, rounded likewise, and
+// the column sums of the unrounded values over 64 rows; VEC = 8: rows of whole aligned 16-byte words.  Bound by memory: a warp has four rows in flight.  The sums of the row
 // blocks are added by a second kernel in a fixed order.
 constexpr int kSumRows = 64;
 struct SlopeParams {
@@ -1024,12 +1024,13 @@ struct SlopeParams {
     const __nv_bfloat16* z;
     int64_t ldz;
     __nv_bfloat16* dz;   // NULL: sums only
-    int64_t lddz;
+    __nv_bfloat16* rest; // dZ - dz, where REST
+    int64_t lddz;        // of both
     float* sums;         // [row blocks][N], NULL: none
     int64_t M, N;
 };
 
-template <int ACT, int VEC>
+template <int ACT, int VEC, bool REST>
 __global__ void __launch_bounds__(256) linear_slope_kernel(const SlopeParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t c = (int64_t)blockIdx.x * 32 * VEC + lane * VEC;
@@ -1063,17 +1064,23 @@ __global__ void __launch_bounds__(256) linear_slope_kernel(const SlopeParams p) 
 #pragma unroll
             for (int k = 0; k < kAtOnce; ++k) {
                 const int64_t r = r0 + i + 8 * k;
-                Word o;
+                Word o, rest;
 #pragma unroll
                 for (int j = 0; j < VEC; ++j) {
                     float v = __bfloat162float(dy[k].h[j]);
                     if (ACT != DASTAC_ACT_NONE) v *= slope_of<ACT>(__bfloat162float(z[k].h[j]));
                     if (r < p.M) sum[j] += v;
                     o.h[j] = __float2bfloat16_rn(v);
+                    // an infinity leaves nothing (and not NaN)
+                    if (REST) rest.h[j] = __float2bfloat16_rn((__bfloat16_as_ushort(o.h[j]) & 0x7f80) == 0x7f80 ? 0.f : v - __bfloat162float(o.h[j]));
                 }
                 if (p.dz && r < p.M) {
                     if (VEC == 8) *(uint4*)(p.dz + r * p.lddz + c) = o.q;
                     else p.dz[r * p.lddz + c] = o.h[0];
+                }
+                if (REST && r < p.M) {
+                    if (VEC == 8) *(uint4*)(p.rest + r * p.lddz + c) = rest.q;
+                    else p.rest[r * p.lddz + c] = rest.h[0];
                 }
             }
         }
@@ -1403,24 +1410,35 @@ dastac_status multiply(const Problem& q, const Operand& P, const Operand& Q, int
     return launch_pair(&q, &m, 1, err_word, st);
 }
 
-template <int VEC>
-void launch_slope(const SlopeParams& p, int act, cudaStream_t st) {
+template <int VEC, bool REST>
+void launch_slope_as(const SlopeParams& p, int act, cudaStream_t st) {
     const dim3 grid((unsigned)((p.N + 32 * VEC - 1) / (32 * VEC)), (unsigned)((p.M + kSumRows - 1) / kSumRows));
     switch (act) {
-        case DASTAC_ACT_RELU: linear_slope_kernel<DASTAC_ACT_RELU, VEC><<<grid, 256, 0, st>>>(p); break;
-        case DASTAC_ACT_SIGMOID: linear_slope_kernel<DASTAC_ACT_SIGMOID, VEC><<<grid, 256, 0, st>>>(p); break;
-        case DASTAC_ACT_SILU: linear_slope_kernel<DASTAC_ACT_SILU, VEC><<<grid, 256, 0, st>>>(p); break;
-        case DASTAC_ACT_GELU: linear_slope_kernel<DASTAC_ACT_GELU, VEC><<<grid, 256, 0, st>>>(p); break;
-        default: linear_slope_kernel<DASTAC_ACT_NONE, VEC><<<grid, 256, 0, st>>>(p); break;
+        case DASTAC_ACT_SIGMOID: linear_slope_kernel<DASTAC_ACT_SIGMOID, VEC, REST><<<grid, 256, 0, st>>>(p); break;
+        case DASTAC_ACT_SILU: linear_slope_kernel<DASTAC_ACT_SILU, VEC, REST><<<grid, 256, 0, st>>>(p); break;
+        case DASTAC_ACT_GELU: linear_slope_kernel<DASTAC_ACT_GELU, VEC, REST><<<grid, 256, 0, st>>>(p); break;
+        // no rest where dZ is dY or 0
+        case DASTAC_ACT_RELU: linear_slope_kernel<DASTAC_ACT_RELU, VEC, false><<<grid, 256, 0, st>>>(p); break;
+        default: linear_slope_kernel<DASTAC_ACT_NONE, VEC, false><<<grid, 256, 0, st>>>(p); break;
     }
 }
+template <int VEC>
+void launch_slope(const SlopeParams& p, int act, cudaStream_t st) {
+    if (p.rest) launch_slope_as<VEC, true>(p, act, st);
+    else launch_slope_as<VEC, false>(p, act, st);
+}
 
-// Where the backward pass keeps things: dZ (with an activation, or when dY is no operand as it lies), the
-// partial column sums, copies of X and W.
+// Where the backward pass keeps things: dZ (with an activation, or when dY is no operand as it lies) and what rounding it
+// leaves, the partial column sums, copies of X and W.
+//
+// With an activation dZ has more bits than an operand of the products holds.  dX and a bf16 dW are rounded as coarsely
+// themselves and take it rounded.  An fp32 dW would have that rounding's error (1.7e-3 of the result, 2048 rows), so it
+// takes a second product, with what the rounding leaves, unless the caller does without: 2.6e-6 (4096 rows, 4096 by 8192,
+// SiLU: 784 us, 505 without).  relu's dZ is dY or 0 and needs none.
 struct BackwardPlan {
-    Operand x, w, dz;
-    bool make_dz;
-    size_t dz_at, sums_at, bytes;
+    Operand x, w, dz, rest;
+    bool make_dz, make_rest;
+    size_t dz_at, rest_at, sums_at, bytes;
     int64_t row_blocks;
 };
 BackwardPlan plan_backward(const dastac_linear_args* a) {
@@ -1432,6 +1450,12 @@ BackwardPlan plan_backward(const dastac_linear_args* a) {
         b.dz.ld = round_up(a->N, 8);
         b.dz_at = b.bytes;
         b.bytes += (size_t)round_up(a->M * b.dz.ld * 2, 256);
+    }
+    b.make_rest = a->dw && a->K > 0 && a->act != DASTAC_ACT_NONE && a->act != DASTAC_ACT_RELU && a->dw_dtype == DASTAC_F32 && !a->round_dz;
+    b.rest = b.dz;
+    if (b.make_rest) {
+        b.rest_at = b.bytes;
+        b.bytes += (size_t)round_up(a->M * b.rest.ld * 2, 256);
     }
     b.row_blocks = (a->M + kSumRows - 1) / kSumRows;
     b.sums_at = b.bytes;
@@ -1513,6 +1537,7 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         s.z = (const __nv_bfloat16*)a->z;
         s.ldz = a->ldz;
         s.dz = b.make_dz ? (__nv_bfloat16*)((char*)workspace + b.dz_at) : nullptr;
+        s.rest = b.make_rest ? (__nv_bfloat16*)((char*)workspace + b.rest_at) : nullptr;
         s.lddz = b.dz.ld;
         s.sums = a->db ? (float*)((char*)workspace + b.sums_at) : nullptr;
         s.M = a->M;
@@ -1522,6 +1547,7 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         else launch_slope<1>(s, a->act, cs);
         if ((st = launch_status()) != DASTAC_OK) return st;
         if (b.make_dz) b.dz.p = s.dz;
+        if (b.make_rest) b.rest.p = s.rest;
         if (a->db) {
             linear_column_sum_kernel<<<(unsigned)((a->N + 31) / 32), 256, 0, cs>>>(s.sums, b.row_blocks, a->N, a->db, a->accumulate);
             if ((st = launch_status()) != DASTAC_OK) return st;
@@ -1552,21 +1578,24 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         const double slim = plan_slim(q[i]).us, pair = pair_us(&q[i], 1);
         apart += slim < pair ? slim : pair;
     }
+    Problem rest = q[n - 1];   // dW's, added to it
+    rest.accumulate = 1;
     if (n < 2 || apart < pair_us(q, n)) {
         for (int i = 0; i < n; ++i)
             if ((st = multiply(q[i], P[i], Q[i], err_word, cs)) != DASTAC_OK) return st;
-        return DASTAC_OK;
+    } else {
+        Maps m[2]{};
+        for (int i = 0; i < 2; ++i)
+            if (!encode_problem(q[i], P[i], Q[i], m[i])) return DASTAC_ERR_CUDA;
+        if (q[1].k_blocks > q[0].k_blocks) {   // the longer contraction first
+            const Problem tq = q[0];
+            const Maps tm = m[0];
+            q[0] = q[1];
+            m[0] = m[1];
+            q[1] = tq;
+            m[1] = tm;
+        }
+        if ((st = launch_pair(q, m, 2, err_word, cs)) != DASTAC_OK) return st;
     }
-    Maps m[2]{};
-    for (int i = 0; i < 2; ++i)
-        if (!encode_problem(q[i], P[i], Q[i], m[i])) return DASTAC_ERR_CUDA;
-    if (q[1].k_blocks > q[0].k_blocks) {   // the longer contraction first
-        const Problem tq = q[0];
-        const Maps tm = m[0];
-        q[0] = q[1];
-        m[0] = m[1];
-        q[1] = tq;
-        m[1] = tm;
-    }
-    return launch_pair(q, m, 2, err_word, cs);
+    return b.make_rest ? multiply(rest, b.rest, b.x, err_word, cs) : DASTAC_OK;
 }

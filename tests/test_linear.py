@@ -296,6 +296,51 @@ def test_fp32_results_of_long_sums(M, N, K):
 
 @gpu
 @pytest.mark.parametrize("act", ACTS[1:])
+@pytest.mark.parametrize("M,N,K,layout", [(1, 8, 8, "plain"), (300, 130, 72, "odd_pitch"), (2000, 264, 200, "plain"), (700, 2600, 1100, "plain")])
+def test_fp32_weight_gradient_behind_an_activation(M, N, K, layout, act):
+    """dZ has more bits than one bf16 number; an fp32 dW is as good as two of them (2^-16 of each term, and as much of the
+    result, the terms' errors being independent)."""
+    gen = torch.Generator().manual_seed(M + act)
+    x, w, dy = (_place(t, layout) for t in (_rand(gen, M, K), _rand(gen, N, K), _rand(gen, M, N)))
+    z = _place(_rand(gen, M, N, scale=1.5), layout)
+    start = _rand(gen, N, K, dtype=torch.float32)
+    for accumulate in (False, True):
+        dx, dw = torch.empty(M, K, dtype=torch.bfloat16, device="cuda"), start.clone()
+        dastac.linear_backward(dy, x, w, act=act, z=z, dx=dx, dw=dw, accumulate=accumulate,
+                               workspace=_ws(dastac.linear_backward_workspace(dy, x, w, act)))
+        X, dZ = _np(x), _np(dy) * _slope(act, _np(z))
+        ref, size = dZ.T @ X + accumulate * _np(start), np.abs(dZ).T @ np.abs(X) + accumulate * np.abs(_np(start))
+        bound = (_sum_error(M) + EPI + 2.0 ** -16) * size + EPI * np.abs(_np(dy)).T @ np.abs(X)
+        # a slope is good to EPI whatever its own size: relative to dY, which is 4 times dZ or less in the 2-norm
+        _check(dw, ref, bound, "dw", 2.0 ** -16 + FOLDED + 4 * EPI)
+    # a bf16 dW, and one that does without the second part, ask for less (relu's dZ has none)
+    half = dastac.linear_backward_workspace(dy, x, w, act, dw_dtype=torch.bfloat16)
+    assert half == dastac.linear_backward_workspace(dy, x, w, act, round_dz=True)
+    assert (half < dastac.linear_backward_workspace(dy, x, w, act)) == (act != dastac.ACT_RELU)
+    coarse, bf16 = torch.empty(N, K, device="cuda"), torch.empty(N, K, dtype=torch.bfloat16, device="cuda")
+    dastac.linear_backward(dy, x, w, act=act, z=z, dx=dx, dw=coarse, round_dz=True, workspace=_ws(half))
+    dastac.linear_backward(dy, x, w, act=act, z=z, dx=dx, dw=bf16, workspace=_ws(half))
+    for dw in (coarse, bf16):
+        assert float((dw.double().cpu() - torch.from_numpy(dZ.T @ X)).norm()) <= 2.0 ** -7 * float(np.linalg.norm(dZ.T @ X))
+
+
+@gpu
+def test_infinite_gradients_stay_infinite_in_an_fp32_weight_gradient():
+    gen = torch.Generator().manual_seed(8)
+    x, w, dy, z = _rand(gen, 200, 40), _rand(gen, 48, 40), _rand(gen, 200, 48), _rand(gen, 200, 48)
+    grads = []
+    for bad in (1.0, float("inf")):
+        dy[3, 5], z[3, 5] = bad, 1.0
+        dw = torch.empty(48, 40, device="cuda")
+        dastac.linear_backward(dy, x, w, act=dastac.ACT_SILU, z=z, dw=dw, workspace=_ws(dastac.linear_backward_workspace(dy, x, w, dastac.ACT_SILU)))
+        grads.append(dw)
+    others = torch.arange(48, device="cuda") != 5
+    assert torch.equal(grads[0][others], grads[1][others])
+    assert torch.equal(grads[1][5], torch.sign(x[3].float()) * float("inf"))
+
+
+@gpu
+@pytest.mark.parametrize("act", ACTS[1:])
 def test_gradients_against_differences(act):
     """<gradient, direction> against central differences of the 64-bit forward pass.  The kept preactivation is
     a rounded one, so the differences are taken of f around it: z enters as x w^T + (z - x w^T)."""
