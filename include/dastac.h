@@ -474,6 +474,9 @@ typedef struct {
 dastac_status dastac_linear_forward_workspace(const dastac_linear_args* a, size_t* bytes);
 dastac_status dastac_linear_forward(const dastac_linear_args* a, void* workspace, size_t workspace_bytes,
                                     int32_t* err_word, void* stream);
+/* Which kernel that call takes on the current device: 0 none (no result), 1 the one for few tiles, with the contraction
+ * split over a cluster, 2 the one on pairs of CTAs.  The choice is by expected time. */
+dastac_status dastac_linear_forward_kernel(const dastac_linear_args* a, int32_t* kernel);
 dastac_status dastac_linear_backward_workspace(const dastac_linear_args* a, size_t* bytes);
 dastac_status dastac_linear_backward(const dastac_linear_args* a, void* workspace, size_t workspace_bytes,
                                      int32_t* err_word, void* stream);

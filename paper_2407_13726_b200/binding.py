@@ -35,7 +35,7 @@ EXPORTS = [
     "dastac_bandmm_split_tf32", "dastac_ttm_split_tf32",
     "dastac_linrec_workspace", "dastac_linrec_forward", "dastac_linrec_backward",
     "dastac_linear_forward_workspace", "dastac_linear_forward", "dastac_linear_backward_workspace",
-    "dastac_linear_backward",
+    "dastac_linear_backward", "dastac_linear_forward_kernel",
 ]
 GATE_VALUE, GATE_LOG, GATE_SIGMOID = 0, 1, 2
 LINREC_CHUNK = 128
@@ -532,6 +532,7 @@ _lib.dastac_linrec_backward.argtypes = [_shape_p, _seq_p, _seq_p, _seq_p, _vp, _
 for _name in ("forward", "backward"):
     getattr(_lib, f"dastac_linear_{_name}_workspace").argtypes = [_linear_p, ctypes.POINTER(ctypes.c_size_t)]
     getattr(_lib, f"dastac_linear_{_name}").argtypes = [_linear_p, _vp, ctypes.c_size_t, _vp, _vp]
+_lib.dastac_linear_forward_kernel.argtypes = [_linear_p, ctypes.POINTER(ctypes.c_int32)]
 # function objects of the same library that take packed blocks
 _packed = ctypes.CDLL(LIB_PATH)
 _block = ctypes.c_char_p

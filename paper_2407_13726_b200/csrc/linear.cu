@@ -1402,9 +1402,10 @@ dastac_status launch_slim(const SlimPlan& plan, const Problem& q, const Operand&
     return launch_status();
 }
 
+bool on_pairs(const Problem& q, const SlimPlan& slim) { return slim.us >= pair_us(&q, 1); }
 dastac_status multiply(const Problem& q, const Operand& P, const Operand& Q, int32_t* err_word, cudaStream_t st) {
     const SlimPlan plan = plan_slim(q);
-    if (plan.us < pair_us(&q, 1)) return launch_slim(plan, q, Q, P, err_word, st);
+    if (!on_pairs(q, plan)) return launch_slim(plan, q, Q, P, err_word, st);
     Maps m{};
     if (!encode_problem(q, P, Q, m)) return DASTAC_ERR_CUDA;
     return launch_pair(&q, &m, 1, err_word, st);
@@ -1465,6 +1466,18 @@ BackwardPlan plan_backward(const dastac_linear_args* a) {
     return b;
 }
 
+Problem forward_problem(const dastac_linear_args* a) {
+    Problem q = problem_of(0, 0, a->M, a->N, a->K, a->y, a->ldy, a->y_dtype);
+    q.act = a->act;
+    q.bias = a->bias;
+    q.residual = a->residual;
+    q.ldr = a->ldr;
+    q.z = (__nv_bfloat16*)a->z;
+    q.ldz = a->ldz;
+    set_alignment(q);
+    return q;
+}
+
 bool workspace_ok(size_t need, const void* w, size_t have) { return need == 0 || (w && have >= need && ((uintptr_t)w & 255) == 0); }
 
 }  // namespace
@@ -1493,15 +1506,18 @@ extern "C" dastac_status dastac_linear_forward(const dastac_linear_args* a, void
     if (!workspace_ok(need, workspace, workspace_bytes)) return DASTAC_ERR_WORKSPACE;
     cudaStream_t cs = (cudaStream_t)stream;
     if ((st = stage(x, workspace, cs)) != DASTAC_OK || (st = stage(w, workspace, cs)) != DASTAC_OK) return st;
-    Problem q = problem_of(0, 0, a->M, a->N, a->K, a->y, a->ldy, a->y_dtype);
-    q.act = a->act;
-    q.bias = a->bias;
-    q.residual = a->residual;
-    q.ldr = a->ldr;
-    q.z = (__nv_bfloat16*)a->z;
-    q.ldz = a->ldz;
-    set_alignment(q);
-    return multiply(q, x, w, err_word ? err_word : device_error_word(), cs);
+    return multiply(forward_problem(a), x, w, err_word ? err_word : device_error_word(), cs);
+}
+
+extern "C" dastac_status dastac_linear_forward_kernel(const dastac_linear_args* a, int32_t* kernel) {
+    const dastac_status st = check_forward(a);
+    if (st != DASTAC_OK) return st;
+    if (!kernel) return DASTAC_ERR_INVALID_ARG;
+    *kernel = 0;
+    if (a->M == 0 || a->N == 0) return DASTAC_OK;
+    const Problem q = forward_problem(a);
+    *kernel = on_pairs(q, plan_slim(q)) ? 2 : 1;
+    return DASTAC_OK;
 }
 
 extern "C" dastac_status dastac_linear_backward_workspace(const dastac_linear_args* a, size_t* bytes) {

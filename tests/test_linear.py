@@ -182,6 +182,95 @@ def test_same_bits_every_time():
             assert torch.equal(first, dastac.linear_forward(x, w, torch.empty(M, N, device="cuda")))
 
 
+# ---- the kernel on pairs of CTAs, which takes products of many tiles ----------------------------------------------
+
+def _torch_f(act, z):
+    if act == dastac.ACT_RELU:
+        return z.clamp(min=0)
+    if act == dastac.ACT_SIGMOID:
+        return torch.sigmoid(z)
+    if act == dastac.ACT_SILU:
+        return z * torch.sigmoid(z)
+    if act == dastac.ACT_GELU:
+        return 0.5 * z * (1 + torch.erf(z / math.sqrt(2)))
+    return z
+
+
+def _kernel_of(x, w, y, act, b, r, z):
+    """The library's choice for this call."""
+    ptr, pitch = (lambda t: 0 if t is None else t.data_ptr()), (lambda t: 0 if t is None else t.stride(0))
+    which = ctypes.c_int32(-1)
+    a = binding._LinearArgs(M=x.shape[0], N=w.shape[0], K=x.shape[1], act=act, y_dtype=int(y.dtype == torch.bfloat16), x=ptr(x), ldx=pitch(x),
+                            w=ptr(w), ldw=pitch(w), bias=ptr(b), residual=ptr(r), ldr=pitch(r), y=ptr(y), ldy=pitch(y), z=ptr(z), ldz=pitch(z))
+    assert binding._lib.dastac_linear_forward_kernel(a, ctypes.byref(which)) == 0
+    return which.value
+
+
+def _forward_on_pairs(M, N, K, act, dtype, full=True, layout="plain", out_layout="plain", in_place=False):
+    gen = torch.Generator().manual_seed(M + 3 * N + 7 * K)
+    x, w = _place(_rand(gen, M, K), layout), _place(_rand(gen, N, K, scale=max(K, 1) ** -0.5), layout)
+    b = _rand(gen, N, dtype=torch.float32) if full else None
+    r = _place(_rand(gen, M, N, dtype=dtype), out_layout) if full else None
+    y = r if in_place else _place(torch.full((M, N), float("nan"), dtype=dtype, device="cuda"), out_layout)
+    z = _place(torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda"), out_layout) if full else None
+    assert _kernel_of(x, w, y, act, b, r, z) == 2
+    X, W = x.double(), w.double()
+    Z = X @ W.T + (b.double() if full else 0)
+    R = r.double().clone() if full else torch.zeros_like(Z)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    dastac.linear_forward(x, w, y, bias=b, act=act, residual=r, z=z, workspace=_ws(dastac.linear_workspace(x, w)), err_word=err)
+    assert int(err.item()) == 0
+    Y = _torch_f(act, Z) + R
+    ez = _sum_error(K) * (X.abs() @ W.abs().T) + EPI * (Z.abs() + 1)
+    ey = 1.2 * ez + EPI * (Y.abs() + R.abs() + 1)
+    results = [(y, Y, ey, dtype)] + ([(z, Z, ez, torch.bfloat16)] if full else [])
+    for out, ref, e, t in results:
+        bound = e + (BF16 * (ref.abs() + e) if t == torch.bfloat16 else 0)
+        over = float(((out.double() - ref).abs() / (bound + 1e-30)).max())   # NaN, where nothing was written, fails as well
+        assert over <= 1.0, over
+        assert float((out.double() - ref).norm()) <= _norm(t, K) * float(ref.norm())
+    return x, w, y
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("N", [1504, 1500, 1501])    # rows of whole 16 bytes, of whole pairs (bf16), of neither
+def test_pairs_activations(N, act, dtype):
+    _forward_on_pairs(1701, N, 136, act, dtype)
+    _forward_on_pairs(1701, N, 136, act, dtype, full=False)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("layout,out_layout", [("pitch16", "pitch16"), ("odd_pitch", "odd_pitch"), ("odd_base", "odd_base"), ("plain", "odd_base")])
+@pytest.mark.parametrize("M,N,K", [(1700, 1512, 72), (2305, 2568, 72), (2305, 2568, 2200)])   # the last two: more tiles than pairs of CTAs
+def test_pairs_strides_and_several_tiles_a_pair(M, N, K, layout, out_layout, dtype):
+    _forward_on_pairs(M, N, K, dastac.ACT_GELU, dtype, layout=layout, out_layout=out_layout)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("K", [0, 1, 64, 65, 512, 513, 1024, 1100, 2048, 2049])   # around the parts of an fp32 sum
+@pytest.mark.parametrize("out_layout", ["plain", "odd_pitch"])
+def test_pairs_lengths_and_residual_in_place(K, out_layout, dtype):
+    _forward_on_pairs(2305, 2568, K, dastac.ACT_SIGMOID, dtype, out_layout=out_layout, in_place=True)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_pairs_keep_what_is_not_finite_and_the_same_bits(dtype):
+    x, w, first = _forward_on_pairs(2305, 2568, 1100, dastac.ACT_NONE, dtype, full=False)
+    ws = _ws(dastac.linear_workspace(x, w))
+    for _ in range(4):
+        assert torch.equal(first, dastac.linear_forward(x, w, torch.empty_like(first), workspace=ws))
+    x[1000], w[7] = float("nan"), float("inf")
+    dirty = dastac.linear_forward(x, w, torch.empty_like(first), workspace=ws)
+    rows, cols = torch.arange(2305, device="cuda") != 1000, torch.arange(2568, device="cuda") != 7
+    assert torch.equal(first[rows][:, cols], dirty[rows][:, cols])
+    assert dirty[1000].isnan().all() and not dirty[:, 7].isfinite().any()
+
+
 def _backward(M, N, K, act, dw_dtype=torch.bfloat16, accumulate=False, layout="plain", out_layout="plain", want="xwb"):
     gen = torch.Generator().manual_seed(11 + M + 3 * N + 7 * K)
     x, w, dy = (_place(t, layout) for t in (_rand(gen, M, K), _rand(gen, N, K, scale=max(K, 1) ** -0.5), _rand(gen, M, N)))
@@ -394,6 +483,13 @@ def test_refusals_do_not_launch():
     assert lib.dastac_linear_forward_workspace(_args(), None) == 1 and lib.dastac_linear_forward_workspace(None, ctypes.byref(n)) == 1
     assert lib.dastac_linear_forward(_args(ldx=73), 8, 1 << 20, None, None) == 7                       # misaligned workspace
     assert dastac.launch_count() == before
+
+
+def test_kernel_query_refuses_what_the_call_refuses():
+    lib, which = binding._lib, ctypes.c_int32(-1)
+    assert lib.dastac_linear_forward_kernel(_args(M=0), ctypes.byref(which)) == 0 and which.value == 0
+    assert lib.dastac_linear_forward_kernel(_args(), None) == 1 and lib.dastac_linear_forward_kernel(None, ctypes.byref(which)) == 1
+    assert lib.dastac_linear_forward_kernel(_args(ldx=71), ctypes.byref(which)) == 4
 
 
 def test_binding_checks_tensors():
