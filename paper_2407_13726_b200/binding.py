@@ -571,21 +571,21 @@ def _code(dtype: torch.dtype) -> int:
     return code
 
 
-def _extents(g: torch.Tensor, offsets: Optional[torch.Tensor], dev: int):
+def _extents(shape: torch.Size, offsets: Optional[torch.Tensor], dev: int):
     """(batch, steps, channels, pointer to the offsets, sequences) of a call."""
     if offsets is None:
-        batch, steps, channels = g.shape
+        batch, steps, channels = shape
         return batch, steps, channels, 0, 0
-    steps, channels = g.shape
+    steps, channels = shape
     assert offsets.get_device() == dev and offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous()
     assert offsets.numel() >= 1
     return 1, steps, channels, offsets.data_ptr(), offsets.numel() - 1
 
 
-def _sequence(t: torch.Tensor, like: torch.Tensor, dev: int) -> bytes:
-    assert t.get_device() == dev and t.shape == like.shape and t.dtype == like.dtype
+def _sequence(t: torch.Tensor, shape: torch.Size, dtype: torch.dtype, dev: int) -> bytes:
+    assert t.get_device() == dev and t.shape == shape and t.dtype is dtype
     st = t.stride()
-    assert st[-1] == 1 or t.shape[-1] <= 1
+    assert st[-1] == 1 or shape[-1] <= 1
     return _SEQ.pack(t.data_ptr(), st[0] if len(st) == 3 else 0, st[-2])
 
 
@@ -650,16 +650,16 @@ def linrec_forward(g: torch.Tensor, x: torch.Tensor, gate: int, out: Optional[to
     """``h_t = a_t h_{t-1} + u_t`` along the steps of ``g`` and ``x`` (batch x steps x channels; with ``offsets``
     steps x channels, sequences packed behind one another), see ``dastac.h`` for the gates.  ``h_last`` and
     ``carries`` are filled when given; a call with one step is a decoding step."""
-    dev = _device_of(g)
-    batch, steps, channels, off, seqs = _extents(g, offsets, dev)
+    dev, shape, dtype = _device_of(g), g.shape, g.dtype
+    batch, steps, channels, off, seqs = _extents(shape, offsets, dev)
     rows = seqs if off else batch
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
     p0, ld0 = _state(h0, rows, channels, dev)
     p1, ld1 = _state(h_last, rows, channels, dev)
     ws, n = _scratch(workspace, dev)
-    st = _launch(_packed.dastac_linrec_forward, dev, _SHAPE.pack(_code(g.dtype), gate, batch, steps, channels, off, seqs),
-                 _sequence(g, g, dev), _sequence(x, g, dev), p0, ld0, _sequence(out, g, dev), p1, ld1,
+    st = _launch(_packed.dastac_linrec_forward, dev, _SHAPE.pack(_code(dtype), gate, batch, steps, channels, off, seqs),
+                 _sequence(g, shape, dtype, dev), _sequence(x, shape, dtype, dev), p0, ld0, _sequence(out, shape, dtype, dev), p1, ld1,
                  _carries(carries, batch, steps, channels, dev), ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linrec_forward")
@@ -673,8 +673,8 @@ def linrec_backward(g: torch.Tensor, x: torch.Tensor, dy: torch.Tensor, gate: in
                     workspace: Optional[torch.Tensor] = None, err_word: Optional[torch.Tensor] = None):
     """Gradients ``(dg, dx)`` of the recurrence (and ``dh0`` when given) from the gradients ``dy`` of its output
     and ``dh_last`` of its last states; ``carries`` as kept by ``linrec_forward`` on the same inputs."""
-    dev = _device_of(g)
-    batch, steps, channels, off, seqs = _extents(g, offsets, dev)
+    dev, shape, dtype = _device_of(g), g.shape, g.dtype
+    batch, steps, channels, off, seqs = _extents(shape, offsets, dev)
     rows = seqs if off else batch
     if dg is None:
         dg = torch.empty_like(g, memory_format=torch.contiguous_format)
@@ -684,9 +684,9 @@ def linrec_backward(g: torch.Tensor, x: torch.Tensor, dy: torch.Tensor, gate: in
     p1, ld1 = _state(dh_last, rows, channels, dev)
     p2, ld2 = _state(dh0, rows, channels, dev)
     ws, n = _scratch(workspace, dev)
-    st = _launch(_packed.dastac_linrec_backward, dev, _SHAPE.pack(_code(g.dtype), gate, batch, steps, channels, off, seqs),
-                 _sequence(g, g, dev), _sequence(x, g, dev), _sequence(dy, g, dev), p0, ld0,
-                 _carries(carries, batch, steps, channels, dev), p1, ld1, _sequence(dg, g, dev), _sequence(dx, g, dev), p2, ld2,
+    st = _launch(_packed.dastac_linrec_backward, dev, _SHAPE.pack(_code(dtype), gate, batch, steps, channels, off, seqs),
+                 _sequence(g, shape, dtype, dev), _sequence(x, shape, dtype, dev), _sequence(dy, shape, dtype, dev), p0, ld0,
+                 _carries(carries, batch, steps, channels, dev), p1, ld1, _sequence(dg, shape, dtype, dev), _sequence(dx, shape, dtype, dev), p2, ld2,
                  ws, n, _error_word(err_word, dev))
     if st:
         raise DastacError(st, "dastac_linrec_backward")
