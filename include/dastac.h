@@ -418,8 +418,8 @@ dastac_status dastac_linrec_backward(const dastac_linrec_shape* shape, const das
  *     Y = f(Z) + R         R: M x N, y_dtype (NULL: none), Y: M x N, y_dtype (f32 or bf16)
  *     dZ = dY f'(Z),  dX = dZ W,  dW = dZ^T X,  db = sum over the rows of dZ   (dR is dY itself)
  *     f: identity, max(z, 0), s(z) = 1 / (1 + exp(-z)), z s(z), z (1 + erf(z / sqrt 2)) / 2
- * Products are bf16 x bf16 with fp32 accumulation; bias, activation and residual are applied in fp32
- * and Y is rounded once.
+ * Products are bf16 x bf16 with fp32 accumulation (for fp32 results in parts of at most 1024 terms, whose
+ * sum is rounded to nearest); bias, activation and residual are applied in fp32 and Y is rounded once.
  *   z         forward: M x N bf16, the preactivation as the backward call reads it (NULL: not kept);
  *             backward: the same, needed unless act is DASTAC_ACT_NONE.
  *   dy        M x N bf16.  With an activation dZ is rounded to bf16 once, as an operand of the products

@@ -118,7 +118,8 @@ struct Problem {
 // stores a row, two columns a thread: whole segments for any pitch.
 //
 // Measured: 8192 rows, 4096 by 8192, GELU with z kept: 371 us, 1480 TFLOP/s, the tensor pipe active for 94 % of
-// the cycles; bound by the tensor cores at the clock that the power limit leaves.
+// the cycles; bound by the tensor cores at the clock that the power limit leaves.  1017 rows, 1000 by 2501, rows not
+// aligned, fp32 result: 20 us, 40 tiles on 74 pairs, each a launch, a pipeline to fill and an epilogue in a row.
 template <bool DIRECT>
 constexpr int kStagesOf = DIRECT ? 7 : 6;
 constexpr int kOperandBytes = 128 * kBlockK * 2;
@@ -654,8 +655,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
 //
 // Measured: 32 rows, 16384 by 4096: 26 us, 5.2 TB/s, bound by memory; 1 row, 4096 by 4096: 9.3 us, 3.6 TB/s,
 // of which 5.1 us are the weights at the rate of a copy and the rest is the launch, the first bytes' latency, the
-// join and the epilogue.  1017 rows, 1000 by 2501, rows not aligned, fp32 result: 20 us, bound by the same, as a
-// whole tile passes through one CTA with nothing behind it.
+// join and the epilogue.  256 and 512 rows, 4096 by 4096: 17 and 26 us, a whole tile through one CTA with nothing behind it.
 constexpr int kSlimEpi = 8, kSlimTma = 8, kSlimMma = 9;   // warps
 constexpr int kSlimThreads = 32 * (kSlimEpi + 2);
 constexpr size_t kSlimMax = 232448 - 2048;
@@ -1304,8 +1304,9 @@ int64_t slim_slots(int dev, int sms, int ranks, int per_sm) {
 
 // Which kernel, and how the slim one is laid out: by the time, in us, that each is expected to take.  The constants
 // are fitted to 72 shapes (1 .. 800 rows, 384 .. 8192 columns, 320 .. 8192 inner), each with every layout: the layout
-// picked is within 0.4 % of the fastest in the mean, 25 % at the worst.  With 4096 x 4096 weights slim takes 11 us
-// (16 rows), 13.8 (128) and 17.4 (256) against 25.5 to 26.8 for the pairs; at 512 rows, 25.9 and 27.5, the two meet.
+// picked is within 0.4 % of the fastest in the mean, 5 % at the worst (all times: profiles/linear_layouts.md).  With
+// 4096 x 4096 weights slim takes 11 us (24 rows), 13.8 (100) and 17.5 (200) against 25.6 to 26.7 for the pairs; at 512 rows,
+// 26.1 and 27.5, the two meet.
 struct SlimPlan {
     int tokens, ranks, stages;
     size_t smem;
@@ -1435,7 +1436,7 @@ void launch_slope(const SlopeParams& p, int act, cudaStream_t st) {
 // With an activation dZ has more bits than an operand of the products holds.  dX and a bf16 dW are rounded as coarsely
 // themselves and take it rounded.  An fp32 dW would have that rounding's error (1.7e-3 of the result, 2048 rows), so it
 // takes a second product, with what the rounding leaves, unless the caller does without: 2.6e-6 (4096 rows, 4096 by 8192,
-// SiLU: 784 us, 505 without).  relu's dZ is dY or 0 and needs none.
+// SiLU, dX and dW: 734 us, 446 without).  relu's dZ is dY or 0 and needs none.
 struct BackwardPlan {
     Operand x, w, dz, rest;
     bool make_dz, make_rest;
@@ -1586,8 +1587,8 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         P[n] = b.dz;
         Q[n++] = b.x;
     }
-    // each by itself, whichever kernel suits it, or both in one launch on the pairs (2001 rows, 520 by 1363:
-    // the call takes 36 us with one launch, 41.5 with two; 4096 rows, 4096 by 8192: 412 and 424)
+    // each by itself, whichever kernel suits it, or both in one launch on the pairs (2001 rows, 520 by 1363: on the GPU
+    // all of it takes 36 us with one launch of products, 41.5 with two; 4096 rows, 4096 by 8192: 412 and 424)
     double apart = 0.0;
     for (int i = 0; i < n; ++i) {
         set_alignment(q[i]);

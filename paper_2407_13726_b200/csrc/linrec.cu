@@ -33,7 +33,8 @@
 // bound it (issue slots 50 to 55 % busy with 20 warps an SM; memory at 82 % of a copy's rate forwards).  With few
 // chains it is the time of a tile: copy, sweep, join and second sweep follow one another, and two CTAs an SM are
 // all there is to overlap them (1 x 65536 steps x 2048 bf16 channels: 254 us, 3.2 TB/s).  Forwards and backwards,
-// 4 x 4096 steps x 2560 bf16 channels: 180 us.
+// 4 x 4096 steps x 2560 bf16 channels: 180 us.  8 x 2048 steps x 2048 fp32 channels: 68 us forwards, 94 backwards.  bf16 rows
+// that split a word are taken element by element: 8 x 2048 steps x 4095 channels: 558 us forwards, 699 backwards.
 #include <cuda_bf16.h>
 
 #include "bf16_mma.cuh"
@@ -147,6 +148,8 @@ __device__ __forceinline__ Pack<2> fma(Pack<2> a, Pack<2> b, Pack<2> c) {
 
 // The gate; for the sigmoid also its complement s(-g) = e s(g) with e = exp(-g), which keeps its relative
 // precision where 1 - s(g) would not.  e stays finite (2^115 at most), NaN passes.
+// The approximate exponential and reciprocal are good to 2^-22: packed fp32 sequences with logarithmic gates come out with
+// 2.9e-7 of their size, 1.4e-7 with gates to the last bit.
 template <int GATE, int N>
 __device__ __forceinline__ Pack<N> exp_of(Pack<N> g) {
     Pack<N> t = g * Pack<N>(GATE == DASTAC_GATE_LOG ? 1.4426950408889634f : -1.4426950408889634f);
