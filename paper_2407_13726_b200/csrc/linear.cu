@@ -1304,9 +1304,8 @@ int64_t slim_slots(int dev, int sms, int ranks, int per_sm) {
 
 // Which kernel, and how the slim one is laid out: by the time, in us, that each is expected to take.  The constants
 // are fitted to 72 shapes (1 .. 800 rows, 384 .. 8192 columns, 320 .. 8192 inner), each with every layout: the layout
-// picked is within 0.4 % of the fastest in the mean, 5 % at the worst (all times: profiles/linear_layouts.md).  With
-// 4096 x 4096 weights slim takes 11 us (24 rows), 13.8 (100) and 17.5 (200) against 25.6 to 26.7 for the pairs; at 512 rows,
-// 26.1 and 27.5, the two meet.
+// picked is within 0.4 % of the fastest in the mean, 5 % at the worst.  With 4096 x 4096 weights slim takes 11 us (24
+// rows), 13.8 (100) and 17.5 (200) against 25.6 to 26.7 for the pairs; at 512 rows, 26.1 and 27.5, the two meet.
 struct SlimPlan {
     int tokens, ranks, stages;
     size_t smem;
