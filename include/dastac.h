@@ -424,9 +424,9 @@ dastac_status dastac_linrec_backward(const dastac_linrec_shape* shape, const das
  *             backward: the same, needed unless act is DASTAC_ACT_NONE.
  *   dy        M x N bf16.  With an activation dZ is rounded to bf16 once, as an operand of the products
  *             (relative error at most 2^-8 per term), for dX and for a bf16 dW.  An fp32 dW takes dZ as the
- *             sum of two bf16 numbers (2^-16 per term) in two products (where x is infinite, dW may be
- *             NaN instead of infinite then), or rounded like the others if round_dz is set, which saves
- *             a product.  db sums the unrounded values.
+ *             sum of two bf16 numbers (2^-16 per term), at twice the operations (where x is infinite, dW
+ *             may be NaN instead of infinite then), or rounded like the others if round_dz is set.  db
+ *             sums the unrounded values.
  *   dx        M x K bf16; dw: N x K of dw_dtype (f32 or bf16); db: N f32; each may be NULL.
  *   accumulate  backward: dw += and db += instead of = (dw_dtype f32 only)
  *   ld*       row pitches in elements, unit stride along a row.  Operands of a product whose base is

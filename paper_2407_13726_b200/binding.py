@@ -764,8 +764,8 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: int
                     accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
                     err_word: Optional[torch.Tensor] = None, round_dz: bool = False) -> None:
     """Fills the gradients that are given: ``dx`` (M x K bf16), ``dw`` (N x K, bf16 or fp32), ``db`` (N fp32);
-    ``accumulate`` adds to ``dw`` (fp32) and ``db``.  With an activation an fp32 ``dw`` takes two products, for the two
-    bf16 parts of dZ; ``round_dz`` leaves the second one out."""
+    ``accumulate`` adds to ``dw`` (fp32) and ``db``.  With an activation an fp32 ``dw`` takes dZ in two bf16 parts, at
+    twice the operations; ``round_dz`` leaves the second one out."""
     (M, K), N, dev = x.shape, w.shape[0], _device_of(x)
     dw_dtype = torch.bfloat16 if dw is None else dw.dtype
     ws, n = _scratch(workspace, dev)

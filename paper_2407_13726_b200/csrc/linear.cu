@@ -91,6 +91,7 @@ __device__ __forceinline__ float slope_of(float z) {
 struct Problem {
     int32_t a_mn, b_mn;                      // the operand's row index is the contiguous one
     int32_t k_blocks, row_blocks, col_blocks;  // blocks of 64, 256 and 256
+    int32_t k_wrap;   // from this k on Q is read from its beginning again (P is two parts behind one another); a_mn and b_mn only
     int32_t act, out_dtype, accumulate;
     int32_t fold;     // pairs: accumulators are added to sums in registers every few blocks of k
     int32_t even, quad, whole, wide;   // out, z and residual take 2 columns, 4 columns, 16 bytes, 32 bytes in an aligned access
@@ -474,7 +475,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
             Turn turn{0, 1};   // a fresh barrier's phase before the first counts as complete
             bool ok = true;
             // the copies of a tile, for each order of the operands
-            auto copy_tile = [&](const CUtensorMap* ma, const CUtensorMap* mb, int ra, int rb, int k_blocks, auto a_mn, auto b_mn) {
+            auto copy_tile = [&](const CUtensorMap* ma, const CUtensorMap* mb, int ra, int rb, int k_blocks, int k_wrap, auto a_mn, auto b_mn) {
                 for (int k = 0; k < k_blocks * kBlockK; k += kBlockK, turn.next(kStages)) {
                     if (!wait_stage(empty(turn.s), turn.parity, abort_flag, p.err_word, kErrEmpty)) return false;
                     const uint32_t dst = smem_base + turn.s * kStageBytes, bar = full0 + 8u * turn.s;
@@ -486,8 +487,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
                         tma_load_2d_pair(dst, ma, k, ra, bar);
                     }
                     if constexpr (b_mn.value) {
-                        tma_load_2d_pair(dst + kOperandBytes, mb, rb, k, bar);
-                        tma_load_2d_pair(dst + kOperandBytes + 8192, mb, rb + 64, k, bar);
+                        const int kq = a_mn.value && k >= k_wrap ? k - k_wrap : k;
+                        tma_load_2d_pair(dst + kOperandBytes, mb, rb, kq, bar);
+                        tma_load_2d_pair(dst + kOperandBytes + 8192, mb, rb + 64, kq, bar);
                     } else {
                         tma_load_2d_pair(dst + kOperandBytes, mb, k, rb, bar);
                     }
@@ -503,9 +505,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant
                 const CUtensorMap* ma = which ? &a1 : &a0;
                 const CUtensorMap* mb = which ? &b1 : &b0;
                 const int ra = R * 256 + (int)rank * 128, rb = C * 256 + (int)rank * 128;
-                if (q.a_mn) ok = copy_tile(ma, mb, ra, rb, q.k_blocks, True{}, True{});
-                else if (q.b_mn) ok = copy_tile(ma, mb, ra, rb, q.k_blocks, False{}, True{});
-                else ok = copy_tile(ma, mb, ra, rb, q.k_blocks, False{}, False{});
+                if (q.a_mn) ok = copy_tile(ma, mb, ra, rb, q.k_blocks, q.k_wrap, True{}, True{});
+                else if (q.b_mn) ok = copy_tile(ma, mb, ra, rb, q.k_blocks, q.k_wrap, False{}, True{});
+                else ok = copy_tile(ma, mb, ra, rb, q.k_blocks, q.k_wrap, False{}, False{});
             }
             if (!ok) {   // give copies in flight time to land before shared memory is released
                 const long long t0 = clock64();
@@ -849,8 +851,9 @@ linear_slim_kernel(const __grid_constant__ CUtensorMap mw, const __grid_constant
                 }
                 mbar_arrive_expect_tx(bar, stage_bytes);
                 if (wide) {
-                    tma_load_2d_local(dst, &mw, (int)n0, k, bar);
-                    tma_load_2d_local(dst + 8192, &mw, (int)n0 + 64, k, bar);
+                    const int kq = k >= q.k_wrap ? k - q.k_wrap : k;
+                    tma_load_2d_local(dst, &mw, (int)n0, kq, bar);
+                    tma_load_2d_local(dst + 8192, &mw, (int)n0 + 64, kq, bar);
                 } else {
                     tma_load_2d_local(dst, &mw, k, (int)n0, bar);
                 }
@@ -1024,7 +1027,7 @@ struct SlopeParams {
     const __nv_bfloat16* z;
     int64_t ldz;
     __nv_bfloat16* dz;   // NULL: sums only
-    __nv_bfloat16* rest; // dZ - dz, where REST
+    __nv_bfloat16* rest; // dZ - dz, where REST: rows in whole blocks of kSumRows, behind those of dz, what lies beyond M zero
     int64_t lddz;        // of both
     float* sums;         // [row blocks][N], NULL: none
     int64_t M, N;
@@ -1074,11 +1077,11 @@ __global__ void __launch_bounds__(256) linear_slope_kernel(const SlopeParams p) 
                     // an infinity leaves nothing (and not NaN)
                     if (REST) rest.h[j] = __float2bfloat16_rn((__bfloat16_as_ushort(o.h[j]) & 0x7f80) == 0x7f80 ? 0.f : v - __bfloat162float(o.h[j]));
                 }
-                if (p.dz && r < p.M) {
+                if (p.dz && (REST || r < p.M)) {
                     if (VEC == 8) *(uint4*)(p.dz + r * p.lddz + c) = o.q;
                     else p.dz[r * p.lddz + c] = o.h[0];
                 }
-                if (REST && r < p.M) {
+                if (REST) {
                     if (VEC == 8) *(uint4*)(p.rest + r * p.lddz + c) = rest.q;
                     else p.rest[r * p.lddz + c] = rest.h[0];
                 }
@@ -1221,6 +1224,7 @@ Problem problem_of(int a_mn, int b_mn, int64_t rows, int64_t cols, int64_t k, vo
     q.rows = rows;
     q.cols = cols;
     q.k_blocks = (int32_t)((k + kBlockK - 1) / kBlockK);
+    q.k_wrap = INT32_MAX;
     q.row_blocks = (int32_t)((rows + 255) / 256);
     q.col_blocks = (int32_t)((cols + 255) / 256);
     q.act = DASTAC_ACT_NONE;
@@ -1433,32 +1437,28 @@ void launch_slope(const SlopeParams& p, int act, cudaStream_t st) {
 // leaves, the partial column sums, copies of X and W.
 //
 // With an activation dZ has more bits than an operand of the products holds.  dX and a bf16 dW are rounded as coarsely
-// themselves and take it rounded.  An fp32 dW would have that rounding's error (1.7e-3 of the result, 2048 rows), so it
-// takes a second product, with what the rounding leaves, unless the caller does without: 2.6e-6 (4096 rows, 4096 by 8192,
-// SiLU, dX and dW: 734 us, 446 without).  relu's dZ is dY or 0 and needs none.
+// themselves and take it rounded.  An fp32 dW would have that rounding's error (1.7e-3 of the result, 2048 rows), so its sum
+// goes on over what the rounding leaves, a second part of dZ behind the first, with the same rows of X, unless the caller
+// does without: 2.6e-6 (4096 rows, 4096 by 8192, SiLU, dX and dW: 650 us, 458 without; as a product of its own that is
+// added to dW: 734).  relu's dZ is dY or 0 and needs none.
 struct BackwardPlan {
-    Operand x, w, dz, rest;
+    Operand x, w, dz;
     bool make_dz, make_rest;
-    size_t dz_at, rest_at, sums_at, bytes;
+    size_t dz_at, sums_at, bytes;
     int64_t row_blocks;
 };
 BackwardPlan plan_backward(const dastac_linear_args* a) {
     BackwardPlan b{};
     const bool products = (a->dx || a->dw) && a->K > 0;
     b.make_dz = products && (a->act != DASTAC_ACT_NONE || !(aligned16(a->dy) && (a->M <= 1 || a->lddy % 8 == 0)));
+    b.make_rest = a->dw && a->K > 0 && a->act != DASTAC_ACT_NONE && a->act != DASTAC_ACT_RELU && a->dw_dtype == DASTAC_F32 && !a->round_dz;
+    b.row_blocks = (a->M + kSumRows - 1) / kSumRows;
     b.dz = Operand{a->dy, a->M, a->N, a->lddy, false, 0};
     if (b.make_dz) {
         b.dz.ld = round_up(a->N, 8);
         b.dz_at = b.bytes;
-        b.bytes += (size_t)round_up(a->M * b.dz.ld * 2, 256);
+        b.bytes += (size_t)round_up((b.make_rest ? 2 * b.row_blocks * kSumRows : a->M) * b.dz.ld * 2, 256);
     }
-    b.make_rest = a->dw && a->K > 0 && a->act != DASTAC_ACT_NONE && a->act != DASTAC_ACT_RELU && a->dw_dtype == DASTAC_F32 && !a->round_dz;
-    b.rest = b.dz;
-    if (b.make_rest) {
-        b.rest_at = b.bytes;
-        b.bytes += (size_t)round_up(a->M * b.rest.ld * 2, 256);
-    }
-    b.row_blocks = (a->M + kSumRows - 1) / kSumRows;
     b.sums_at = b.bytes;
     if (a->db) b.bytes += (size_t)round_up(b.row_blocks * a->N * 4, 256);
     b.w = operand_of(a->w, a->dx ? a->N : 0, a->K, a->ldw, b.bytes);
@@ -1553,7 +1553,7 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         s.z = (const __nv_bfloat16*)a->z;
         s.ldz = a->ldz;
         s.dz = b.make_dz ? (__nv_bfloat16*)((char*)workspace + b.dz_at) : nullptr;
-        s.rest = b.make_rest ? (__nv_bfloat16*)((char*)workspace + b.rest_at) : nullptr;
+        s.rest = b.make_rest ? s.dz + b.row_blocks * kSumRows * b.dz.ld : nullptr;
         s.lddz = b.dz.ld;
         s.sums = a->db ? (float*)((char*)workspace + b.sums_at) : nullptr;
         s.M = a->M;
@@ -1563,7 +1563,6 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         else launch_slope<1>(s, a->act, cs);
         if ((st = launch_status()) != DASTAC_OK) return st;
         if (b.make_dz) b.dz.p = s.dz;
-        if (b.make_rest) b.rest.p = s.rest;
         if (a->db) {
             linear_column_sum_kernel<<<(unsigned)((a->N + 31) / 32), 256, 0, cs>>>(s.sums, b.row_blocks, a->N, a->db, a->accumulate);
             if ((st = launch_status()) != DASTAC_OK) return st;
@@ -1581,9 +1580,15 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         Q[n++] = b.w;
     }
     if (a->dw) {
-        q[n] = problem_of(1, 1, a->N, a->K, a->M, a->dw, a->lddw, a->dw_dtype);
+        static_assert(kSumRows % kBlockK == 0, "the second part begins with a block of k");
+        const int64_t part = b.row_blocks * kSumRows;
+        q[n] = problem_of(1, 1, a->N, a->K, b.make_rest ? 2 * part : a->M, a->dw, a->lddw, a->dw_dtype);
         q[n].accumulate = a->accumulate;
         P[n] = b.dz;
+        if (b.make_rest) {
+            P[n].rows = 2 * part;
+            q[n].k_wrap = (int32_t)part;
+        }
         Q[n++] = b.x;
     }
     // each by itself, whichever kernel suits it, or both in one launch on the pairs (2001 rows, 520 by 1363: on the GPU
@@ -1594,24 +1599,21 @@ extern "C" dastac_status dastac_linear_backward(const dastac_linear_args* a, voi
         const double slim = plan_slim(q[i]).us, pair = pair_us(&q[i], 1);
         apart += slim < pair ? slim : pair;
     }
-    Problem rest = q[n - 1];   // dW's, added to it
-    rest.accumulate = 1;
     if (n < 2 || apart < pair_us(q, n)) {
         for (int i = 0; i < n; ++i)
             if ((st = multiply(q[i], P[i], Q[i], err_word, cs)) != DASTAC_OK) return st;
-    } else {
-        Maps m[2]{};
-        for (int i = 0; i < 2; ++i)
-            if (!encode_problem(q[i], P[i], Q[i], m[i])) return DASTAC_ERR_CUDA;
-        if (q[1].k_blocks > q[0].k_blocks) {   // the longer contraction first
-            const Problem tq = q[0];
-            const Maps tm = m[0];
-            q[0] = q[1];
-            m[0] = m[1];
-            q[1] = tq;
-            m[1] = tm;
-        }
-        if ((st = launch_pair(q, m, 2, err_word, cs)) != DASTAC_OK) return st;
+        return DASTAC_OK;
     }
-    return b.make_rest ? multiply(rest, b.rest, b.x, err_word, cs) : DASTAC_OK;
+    Maps m[2]{};
+    for (int i = 0; i < 2; ++i)
+        if (!encode_problem(q[i], P[i], Q[i], m[i])) return DASTAC_ERR_CUDA;
+    if (q[1].k_blocks > q[0].k_blocks) {   // the longer contraction first
+        const Problem tq = q[0];
+        const Maps tm = m[0];
+        q[0] = q[1];
+        m[0] = m[1];
+        q[1] = tq;
+        m[1] = tm;
+    }
+    return launch_pair(q, m, 2, err_word, cs);
 }
