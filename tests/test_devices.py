@@ -54,8 +54,7 @@ def library(monkeypatch):
     monkeypatch.setattr(torch.cuda, "device", device)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: state[0])
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 70 + dev)
-    if hasattr(binding._linrec_bytes, "cache_clear"):
-        binding._linrec_bytes.cache_clear()
+    binding._linrec_bytes.cache_clear()
     yield lib
     assert state[0] == 0
     binding._linrec_bytes.cache_clear()
